@@ -66,7 +66,8 @@ typedef enum thc_status {
 } thc_status;
 
 enum { THC_MAX_WORKERS = 64 };
-enum { THC_DTYPE_F32 = 0, THC_DTYPE_BF16 = 1 };
+enum { THC_DTYPE_F32 = 0, THC_DTYPE_BF16 = 1,
+       THC_DTYPE_F16 = 2 /* tensors of a thc_tensors list only: thc_params.in_dtype does not take it */ };
 
 /* Order in which the butterfly stages of the Hadamard transform run (each stage pairs coordinates whose
  * offsets inside the block differ in one bit).  Every order computes the same transform; in binary32 the
@@ -205,6 +206,58 @@ int thc_uniform_compress(const thc_params* p, uint32_t worker_id, uint64_t round
 /* Alg. 1's estimate m + (1/n) X (M - m)/(2^b - 1) from the aggregated sums X (then RHT^-1 when rotate != 0). */
 int thc_uniform_decompress(const thc_params* p, uint64_t round, const void* agg, int rotate,
                            const float* range_m, const float* range_M, float* out, void* ws, void* stream);
+
+/* ---- a model's tensors ------------------------------------------------------------------------------
+ * A model's gradient is a list of tensors; the calls above take one flat, padded vector per worker.  These calls
+ * stand between the two: the global norm of a list and the factor that clips by it, clipping in place, gathering
+ * the list into the flat vector (with that factor on the way), and scattering an estimate over the list.  Same
+ * stream, workspace and error conventions as above; all of them can be captured into a HIP graph (the list
+ * travels by value with the launches, so the arrays of thc_tensors are read during the call only).
+ *
+ * A list may hold up to 2^40 - 1 elements.  Every tensor is one run of memory, aligned to its own element type,
+ * and is taken in the order of its memory.  Tensors without elements are allowed (their pointer may be null). */
+typedef struct thc_tensors {
+  uint64_t count;
+  void* const* data;     /* host array of device pointers */
+  const uint64_t* numel; /* host array: elements of each tensor */
+  const uint32_t* dtype; /* host array: THC_DTYPE_F32, THC_DTYPE_BF16 or THC_DTYPE_F16, each by itself */
+} thc_tensors;
+
+/* Which norm: the square root of the sum of all squares, or the largest magnitude. */
+enum { THC_NORM_L2 = 0, THC_NORM_MAX = 1 };
+
+/* Bytes of device workspace of thc_grad_norm and thc_grad_clip (the same for every list). */
+int thc_norm_workspace_bytes(size_t* bytes_out /* host */);
+
+/* Global norm v over all elements of the list, and the factor that clips by it.
+ *   max_norm   >= 0, may be infinite.
+ *   norm_out   device, one float, written: v rounded once.  Squares are added up in binary64 in a fixed order (the
+ *              same list at the same addresses modulo 128 bytes gives the same bits).  NaN if any element is NaN,
+ *              else infinite if any element is, or if v exceeds binary32 (the factor then still goes by v itself).
+ *   scale_out  device, one float, written, or NULL: 1 where v <= max_norm, else max_norm / v rounded once (0 for
+ *              infinite elements, NaN for NaN).
+ * An empty list has norm 0 and factor 1.  To clip by a norm that covers more than this list (other processes'
+ * shards), combine the norms and hand the factor to thc_gather or thc_scatter. */
+int thc_grad_norm(const thc_tensors* t, int kind, float max_norm, float* norm_out, float* scale_out /* or NULL */,
+                  void* ws, void* stream);
+
+/* thc_grad_norm, and every element multiplied by the factor in binary32 and rounded to its type, in place.  Where
+ * the factor is 1 nothing is written.  Tensors must not overlap each other (THC_EINVAL: a tensor listed twice would
+ * be scaled twice). */
+int thc_grad_clip(const thc_tensors* t, int kind, float max_norm, float* norm_out, float* scale_out /* or NULL */,
+                  void* ws, void* stream);
+
+/* The list's elements one tensor after another, times *scale (binary32 product, rounded to p->in_dtype), then zeros
+ * up to p->d: a worker's gradient for the calls above.  Of `p` only d and in_dtype matter to the result.
+ *   scale      device, one float, or NULL for 1.
+ *   grad_out   device, d values of in_dtype, 16-byte aligned, written; must not overlap the tensors (THC_EINVAL).
+ * A list of more than d elements is refused (THC_EINVAL). */
+int thc_gather(const thc_params* p, const thc_tensors* t, const float* scale /* or NULL */, void* grad_out, void* stream);
+
+/* The other way: each tensor gets its part of `flat` (d binary32 values, as thc_decompress writes them), times *scale,
+ * rounded to the tensor's type.  Tensors must overlap neither each other nor `flat` (THC_EINVAL). */
+int thc_scatter(const thc_params* p, const float* flat, const float* scale /* or NULL */, const thc_tensors* t,
+                void* stream);
 
 /* ---- host-side helpers (no GPU work) ------------------------------------------------------------- */
 

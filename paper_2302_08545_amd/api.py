@@ -10,14 +10,16 @@ _LIB = None
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libthc.so")
 
 THC_MAX_WORKERS = 64
-THC_DTYPE_F32, THC_DTYPE_BF16 = 0, 1
+THC_DTYPE_F32, THC_DTYPE_BF16, THC_DTYPE_F16 = 0, 1, 2
+THC_NORM_L2, THC_NORM_MAX = 0, 1
 THC_ORDER_ASCENDING, THC_ORDER_SPLIT = 0, 1
 
 EXPORTS = ("thc_version", "thc_strerror", "thc_workspace_bytes", "thc_prepare_range", "thc_compress",
            "thc_compress_all", "thc_aggregate", "thc_decompress", "thc_decompress_noalloc",
            "thc_uniform_workspace_bytes",
            "thc_uniform_prepare_range", "thc_uniform_compress", "thc_uniform_decompress", "thc_threshold",
-           "thc_solve_table", "thc_solve_table_bruteforce", "thc_describe_plan")
+           "thc_solve_table", "thc_solve_table_bruteforce", "thc_describe_plan", "thc_norm_workspace_bytes",
+           "thc_grad_norm", "thc_grad_clip", "thc_gather", "thc_scatter")
 
 
 class thc_params(C.Structure):
@@ -25,6 +27,14 @@ class thc_params(C.Structure):
                 ("g", C.c_uint32), ("agg_bits", C.c_uint32), ("in_dtype", C.c_uint32), ("t_p", C.c_float),
                 ("seed", C.c_uint64), ("table", C.c_uint8 * 256), ("stage_order", C.c_uint32),
                 ("first_block", C.c_uint32), ("group_log2", C.c_uint32), ("single_launch", C.c_uint32)]
+
+
+class thc_tensors(C.Structure):
+    """A list of tensors as the library takes it; made by make_tensors, which keeps the tensors and their device with it."""
+    _fields_ = [("count", C.c_uint64), ("data", C.POINTER(C.c_void_p)), ("numel", C.POINTER(C.c_uint64)),
+                ("dtype", C.POINTER(C.c_uint32))]
+    tensors: tuple = ()
+    device: Optional[int] = None
 
 
 class ThcError(RuntimeError):
@@ -63,6 +73,12 @@ def lib():
         L.thc_solve_table_bruteforce.argtypes = [u32, u32, C.c_double, C.POINTER(C.c_uint8), C.POINTER(C.c_double),
                                                  C.POINTER(C.c_uint64)]
         L.thc_describe_plan.argtypes = [pp, C.POINTER(C.c_uint32), C.c_size_t]
+        pt, f32 = C.POINTER(thc_tensors), C.c_float
+        L.thc_norm_workspace_bytes.argtypes = [C.POINTER(C.c_size_t)]
+        L.thc_grad_norm.argtypes = [pt, C.c_int, f32, vp, vp, vp, vp]
+        L.thc_grad_clip.argtypes = [pt, C.c_int, f32, vp, vp, vp, vp]
+        L.thc_gather.argtypes = [pp, pt, vp, vp, vp]
+        L.thc_scatter.argtypes = [pp, vp, vp, pt, vp]
         _LIB = L
     return _LIB
 
@@ -180,6 +196,123 @@ def thc_uniform_decompress(p: thc_params, rnd: int, agg, rotate: bool, range_m, 
                            stream=None) -> None:
     _check(lib().thc_uniform_decompress(C.byref(p), rnd, _ptr(agg), int(rotate), _ptr(range_m), _ptr(range_M),
                                         _ptr(out), _ptr(ws), _stream(stream)), "thc_uniform_decompress")
+
+
+# ---- a model's tensors -----------------------------------------------------------------------------
+_DTYPES = {}       # torch's types, filled on first use: importing this module does not import torch
+
+
+def _dtypes():
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.float32: THC_DTYPE_F32, torch.bfloat16: THC_DTYPE_BF16, torch.float16: THC_DTYPE_F16})
+    return _DTYPES
+
+
+def _one_run(t) -> bool:
+    """Whether a tensor's elements lie in one run of memory, whatever the order of its dimensions."""
+    if t.is_contiguous():
+        return True
+    at = 1
+    for stride, size in sorted((st, n) for st, n in zip(t.stride(), t.shape) if n != 1):
+        if stride != at:
+            return False
+        at *= size
+    return True
+
+
+def make_tensors(tensors: Sequence) -> thc_tensors:
+    """Describes a list of GPU tensors (float32, bfloat16, float16; any mixture) for the calls below.
+
+    Each tensor is taken in the order of its memory, so it has to be one run of memory: contiguous, or with its
+    dimensions in another order (channels last, transposed).  The list holds the tensors and the addresses that they
+    have now: keep it as long as they stay where they are, and make a new one when a gradient is replaced."""
+    import torch
+    ts, types = tuple(tensors), _dtypes()
+    n, device = len(ts), None
+    for t in ts:
+        if not isinstance(t, torch.Tensor) or t.layout != torch.strided or not t.is_cuda or t.dtype not in types:
+            raise ValueError("make_tensors: takes float32, bfloat16 and float16 tensors on the GPU")
+        if device is not None and t.get_device() != device:
+            raise ValueError("make_tensors: all tensors have to be on one device")
+        device = t.get_device()
+        if not _one_run(t):
+            raise ValueError(f"make_tensors: a tensor of shape {tuple(t.shape)} with strides {tuple(t.stride())} is not one "
+                             "run of memory")
+    out = thc_tensors(n, (C.c_void_p * n)(*[t.data_ptr() for t in ts]), (C.c_uint64 * n)(*[t.numel() for t in ts]),
+                      (C.c_uint32 * n)(*[types[t.dtype] for t in ts]))
+    out.tensors, out.device = ts, device
+    return out
+
+
+def _listed(tensors, stream, where: str) -> thc_tensors:
+    """The list as the library takes it.  A call that goes to the current stream needs it on the current device."""
+    t = tensors if isinstance(tensors, thc_tensors) else make_tensors(tensors)
+    if stream is None and t.device is not None:
+        import torch
+        if torch.cuda.current_device() != t.device:
+            raise ValueError(f"{where}: the tensors are on cuda:{t.device}, the current device is "
+                             f"cuda:{torch.cuda.current_device()}")
+    return t
+
+
+def _buffer(b, name: str, where: str, count: int, dtype=None) -> Optional[int]:
+    """The address of a tensor that has to hold `count` elements of a type (None: bytes) in one run; addresses as they are."""
+    if b is None or isinstance(b, int):
+        return b
+    if dtype is None:
+        ok = b.numel() * b.element_size() >= count
+    else:
+        ok = _dtypes().get(b.dtype) == dtype and b.numel() >= count
+    if not ok or not b.is_cuda or not b.is_contiguous():
+        raise ValueError(f"{where}: {name} has to be a contiguous tensor on the GPU with room for {count} "
+                         f"{'bytes' if dtype is None else 'values of its type'}")
+    return b.data_ptr()
+
+
+_NORM_WS = 0
+
+
+def thc_norm_workspace_bytes() -> int:
+    out = C.c_size_t(0)
+    _check(lib().thc_norm_workspace_bytes(C.byref(out)), "thc_norm_workspace_bytes")
+    return out.value
+
+
+def _norm_call(name: str, tensors, kind, max_norm, norm_out, scale_out, ws, stream) -> None:
+    global _NORM_WS
+    if not _NORM_WS:
+        _NORM_WS = thc_norm_workspace_bytes()
+    t = _listed(tensors, stream, name)
+    _check(getattr(lib(), name)(C.byref(t), kind, max_norm, _buffer(norm_out, "norm_out", name, 1, THC_DTYPE_F32),
+                                _buffer(scale_out, "scale_out", name, 1, THC_DTYPE_F32), _buffer(ws, "ws", name, _NORM_WS),
+                                _stream(stream)), name)
+
+
+def thc_grad_norm(tensors, kind: int, max_norm: float, norm_out, scale_out, ws, stream=None) -> None:
+    """Global norm of a list of tensors (thc_tensors, or a sequence of tensors) and, unless scale_out is None, the factor
+    that clips it to max_norm; both are one float32 on the GPU."""
+    _norm_call("thc_grad_norm", tensors, kind, max_norm, norm_out, scale_out, ws, stream)
+
+
+def thc_grad_clip(tensors, kind: int, max_norm: float, norm_out, scale_out, ws, stream=None) -> None:
+    """thc_grad_norm, and the tensors scaled in place where the norm exceeds max_norm."""
+    _norm_call("thc_grad_clip", tensors, kind, max_norm, norm_out, scale_out, ws, stream)
+
+
+def thc_gather(p: thc_params, tensors, scale, grad_out, stream=None) -> None:
+    """The tensors one after another into the padded vector grad_out (p.d values of p.in_dtype), times *scale (None: 1)."""
+    t = _listed(tensors, stream, "thc_gather")
+    _check(lib().thc_gather(C.byref(p), C.byref(t), _buffer(scale, "scale", "thc_gather", 1, THC_DTYPE_F32),
+                            _buffer(grad_out, "grad_out", "thc_gather", p.d, p.in_dtype), _stream(stream)), "thc_gather")
+
+
+def thc_scatter(p: thc_params, flat, scale, tensors, stream=None) -> None:
+    """The estimate `flat` (p.d float32 values) over the tensors, times *scale (None: 1)."""
+    t = _listed(tensors, stream, "thc_scatter")
+    _check(lib().thc_scatter(C.byref(p), _buffer(flat, "flat", "thc_scatter", p.d, THC_DTYPE_F32),
+                             _buffer(scale, "scale", "thc_scatter", 1, THC_DTYPE_F32), C.byref(t), _stream(stream)),
+           "thc_scatter")
 
 
 def thc_threshold(p: float) -> float:
