@@ -245,26 +245,32 @@ def make_tensors(tensors: Sequence) -> thc_tensors:
     return out
 
 
-def _listed(tensors, stream, where: str) -> thc_tensors:
-    """The list as the library takes it.  A call that goes to the current stream needs it on the current device."""
-    t = tensors if isinstance(tensors, thc_tensors) else make_tensors(tensors)
-    if stream is None and t.device is not None:
-        import torch
-        if torch.cuda.current_device() != t.device:
-            raise ValueError(f"{where}: the tensors are on cuda:{t.device}, the current device is "
-                             f"cuda:{torch.cuda.current_device()}")
-    return t
+def _list_and_stream(tensors, stream, where: str):
+    """The list as the library takes it, and the stream's handle.  The current stream is the current device's: the tensors
+    have to be there too."""
+    t = tensors if type(tensors) is thc_tensors else make_tensors(tensors)
+    if stream is None:
+        if t.device is not None:
+            import torch
+            try:
+                current = torch._C._cuda_getDevice()
+            except AttributeError:
+                current = torch.cuda.current_device()
+            if current != t.device:
+                raise ValueError(f"{where}: the tensors are on cuda:{t.device}, the current device is cuda:{current}")
+        return t, _stream(None)
+    return t, _stream(stream)
 
 
 def _buffer(b, name: str, where: str, count: int, dtype=None) -> Optional[int]:
-    """The address of a tensor that has to hold `count` elements of a type (None: bytes) in one run; addresses as they are."""
+    """The address of a tensor on the GPU that has to hold `count` elements of a type (None: bytes) in one run; addresses as they are."""
     if b is None or isinstance(b, int):
         return b
     if dtype is None:
         ok = b.numel() * b.element_size() >= count
     else:
         ok = _dtypes().get(b.dtype) == dtype and b.numel() >= count
-    if not ok or not b.is_cuda or not b.is_contiguous():
+    if not (ok and b.is_cuda and b.is_contiguous()):
         raise ValueError(f"{where}: {name} has to be a contiguous tensor on the GPU with room for {count} "
                          f"{'bytes' if dtype is None else 'values of its type'}")
     return b.data_ptr()
@@ -279,40 +285,40 @@ def thc_norm_workspace_bytes() -> int:
     return out.value
 
 
-def _norm_call(name: str, tensors, kind, max_norm, norm_out, scale_out, ws, stream) -> None:
+def _norm_call(call, where: str, tensors, kind, max_norm, norm_out, scale_out, ws, stream) -> None:
     global _NORM_WS
     if not _NORM_WS:
         _NORM_WS = thc_norm_workspace_bytes()
-    t = _listed(tensors, stream, name)
-    _check(getattr(lib(), name)(C.byref(t), kind, max_norm, _buffer(norm_out, "norm_out", name, 1, THC_DTYPE_F32),
-                                _buffer(scale_out, "scale_out", name, 1, THC_DTYPE_F32), _buffer(ws, "ws", name, _NORM_WS),
-                                _stream(stream)), name)
+    t, stream = _list_and_stream(tensors, stream, where)
+    rc = call(t, kind, max_norm, _buffer(norm_out, "norm_out", where, 1, THC_DTYPE_F32),
+              _buffer(scale_out, "scale_out", where, 1, THC_DTYPE_F32), _buffer(ws, "ws", where, _NORM_WS), stream)
+    if rc != 0:
+        raise ThcError(rc, where)
 
 
 def thc_grad_norm(tensors, kind: int, max_norm: float, norm_out, scale_out, ws, stream=None) -> None:
     """Global norm of a list of tensors (thc_tensors, or a sequence of tensors) and, unless scale_out is None, the factor
     that clips it to max_norm; both are one float32 on the GPU."""
-    _norm_call("thc_grad_norm", tensors, kind, max_norm, norm_out, scale_out, ws, stream)
+    _norm_call((_LIB or lib()).thc_grad_norm, "thc_grad_norm", tensors, kind, max_norm, norm_out, scale_out, ws, stream)
 
 
 def thc_grad_clip(tensors, kind: int, max_norm: float, norm_out, scale_out, ws, stream=None) -> None:
     """thc_grad_norm, and the tensors scaled in place where the norm exceeds max_norm."""
-    _norm_call("thc_grad_clip", tensors, kind, max_norm, norm_out, scale_out, ws, stream)
+    _norm_call((_LIB or lib()).thc_grad_clip, "thc_grad_clip", tensors, kind, max_norm, norm_out, scale_out, ws, stream)
 
 
 def thc_gather(p: thc_params, tensors, scale, grad_out, stream=None) -> None:
     """The tensors one after another into the padded vector grad_out (p.d values of p.in_dtype), times *scale (None: 1)."""
-    t = _listed(tensors, stream, "thc_gather")
-    _check(lib().thc_gather(C.byref(p), C.byref(t), _buffer(scale, "scale", "thc_gather", 1, THC_DTYPE_F32),
-                            _buffer(grad_out, "grad_out", "thc_gather", p.d, p.in_dtype), _stream(stream)), "thc_gather")
+    t, stream = _list_and_stream(tensors, stream, "thc_gather")
+    _check((_LIB or lib()).thc_gather(p, t, _buffer(scale, "scale", "thc_gather", 1, THC_DTYPE_F32),
+                                      _buffer(grad_out, "grad_out", "thc_gather", p.d, p.in_dtype), stream), "thc_gather")
 
 
 def thc_scatter(p: thc_params, flat, scale, tensors, stream=None) -> None:
     """The estimate `flat` (p.d float32 values) over the tensors, times *scale (None: 1)."""
-    t = _listed(tensors, stream, "thc_scatter")
-    _check(lib().thc_scatter(C.byref(p), _buffer(flat, "flat", "thc_scatter", p.d, THC_DTYPE_F32),
-                             _buffer(scale, "scale", "thc_scatter", 1, THC_DTYPE_F32), C.byref(t), _stream(stream)),
-           "thc_scatter")
+    t, stream = _list_and_stream(tensors, stream, "thc_scatter")
+    _check((_LIB or lib()).thc_scatter(p, _buffer(flat, "flat", "thc_scatter", p.d, THC_DTYPE_F32),
+                                       _buffer(scale, "scale", "thc_scatter", 1, THC_DTYPE_F32), t, stream), "thc_scatter")
 
 
 def thc_threshold(p: float) -> float:

@@ -11,24 +11,40 @@
 
 namespace thc {
 
-// The work of a launch is counted in units of UNIT elements.  A tensor's units lie on a grid that starts on a 128-byte line of
-// what the kernel accesses in whole lines (its own memory, or its place in the flat vector), up to one line before its first
+// The work of a launch is counted in units of a power of two of bytes.  A tensor's units lie on a grid that starts on a 128-byte
+// line of what the kernel accesses in whole lines (its own memory, or its place in the flat vector), up to one line before its first
 // element, so that no line but a tensor's first and last is shared by two units.
-constexpr uint32_t LOG_UNIT = 13, UNIT = 1u << LOG_UNIT;
 constexpr uint32_t LINE = 128;
+constexpr uint32_t LOG_NORM_UNIT = 15, LOG_MOVE_UNIT = 13, LOG_WAVE_UNIT = 12;
 
-// Tensors of one launch, passed by value (a captured graph keeps them): a kernel's arguments have to stay within 4 KB.
-constexpr uint32_t TABLE = 192;
+// A launch holds fewer than 2^32 threads, 2^24 workgroups of 256: longer lists take several, and longer tensors several places in
+// the table, of whole lines.
+constexpr uint32_t MOST_UNITS = 1u << 23;
+constexpr uint64_t MOST_NUMEL = 1ull << 33;
+static_assert((MOST_NUMEL * 4 >> LOG_MOVE_UNIT) < MOST_UNITS);
+
+// Tensors of one launch, passed by value (a captured graph keeps them): a kernel's arguments have to stay within 4 KB.  Short lists
+// travel in a table of their own: a third of the arguments to write and, per wave, of the places to look at.
+constexpr uint32_t TABLE = 192, SHORT_TABLE = 64;
 constexpr int AT_BITS = 40;
 constexpr uint64_t AT_MASK = (1ull << AT_BITS) - 1;
 enum { TYPE_F32 = THC_DTYPE_F32, TYPE_BF16 = THC_DTYPE_BF16, TYPE_F16 = THC_DTYPE_F16, TYPE_ZEROS = 3 };
 
+template <uint32_t N>
 struct TensorTable {
-  void* ptr[TABLE];
-  uint64_t at[TABLE + 1];     // first element's place in the flat vector, and above AT_BITS the tensor's type
-  uint32_t unit[TABLE + 1];   // first unit; behind the last tensor the number of units
+  static constexpr uint32_t SIZE = N;
+  void* ptr[N];
+  uint64_t at[N + 1];     // first element's place in the flat vector, and above AT_BITS the tensor's type
+  uint32_t unit[N + 1];   // first unit; behind the last tensor the number of units
   uint32_t count;
 };
+
+inline void shorten(const TensorTable<TABLE>& from, TensorTable<SHORT_TABLE>* to) {
+  std::copy(from.ptr, from.ptr + from.count, to->ptr);
+  std::copy(from.at, from.at + from.count + 1, to->at);
+  std::copy(from.unit, from.unit + from.count + 1, to->unit);
+  to->count = from.count;
+}
 
 inline uint32_t type_bytes(uint32_t type) { return type == TYPE_F32 ? 4 : 2; }
 
@@ -43,6 +59,25 @@ inline int validate_tensors(const thc_tensors* t, uint64_t* total) {
     if (*total > AT_MASK) return THC_EINVAL;
   }
   return THC_OK;
+}
+
+inline uint64_t list_bytes(const thc_tensors* t) {
+  uint64_t bytes = 0;
+  for (uint64_t i = 0; i < t->count; ++i) bytes += t->numel[i] * type_bytes(t->dtype[i]);
+  return bytes;
+}
+
+// Bytes at the start of a list that the norm's pass reads with plain loads, so that the 256 MB memory-side cache holds them for the
+// call that moves the list next; the rest is read non-temporally, which is 10 % faster and does not push out what is kept.
+// us on one binary32 tensor, nothing kept / 256 MB kept / all kept:
+//              48 MB                  96 MB                  224 MB                  320 MB                  512 MB                 1 GB
+//   norm      13.0 / 13.5            20.2 / 21.9            40.5 / 44.5             55.0 / 59.1 / 60.9      84.6 / 86.2 / 94.6     162 / 163 / 182
+//   + gather  31.4 / 29.0            53.9 / 50.6           115.5 / 109.4           161.6 / 152.8 / 154.7   256.4 / 244.0 / 254.3   508 / 497 / 511
+//   clip      32.7 / 33.0 (16 MB 17.7 / 20.2)  54.5 / 53.4  116.6 / 111.4          164.0 / 154.3 / 156.7   259.6 / 247.2 / 253.0   511 / 501 / 509
+// 384 MB kept: 1 GB 493 (gather) and 494, 512 MB 244.4 and 244.3 but the norm itself 90.1, 320 MB 154.9 and 156.7.
+inline uint64_t norm_keeps(uint64_t bytes, bool in_place) {
+  if (in_place && bytes < 64ull << 20) return 0;
+  return (bytes >= 768ull << 20 ? 384ull : 256ull) << 20;
 }
 
 // Whether memory that a call writes overlaps other memory of the call: the tensors each other (`each_other`), or the range
@@ -80,10 +115,10 @@ enum class Grid { TENSOR, FLAT };
 
 // The tables of a call, one after another: launch(table, units of the table).  Tensors without elements take no place, and one
 // that starts where the one before it ends, with the same type, is part of it.  `zeros`: that many zeros follow the last tensor
-// in the flat vector.  `flat_bytes`: bytes per element of the flat vector (Grid::FLAT).
+// in the flat vector.  `flat_bytes`: bytes per element of the flat vector (Grid::FLAT).  `log_unit`: of a unit's bytes.
 template <class Launch>
-inline void for_tables(const thc_tensors* t, Grid grid, uint32_t flat_bytes, uint64_t zeros, Launch&& launch) {
-  TensorTable tab;
+inline void for_tables(const thc_tensors* t, Grid grid, uint32_t flat_bytes, uint64_t zeros, uint32_t log_unit, Launch&& launch) {
+  TensorTable<TABLE> tab;
   uint32_t k = 0, units = 0;
   uint64_t at = 0;
   auto flush = [&] {
@@ -94,17 +129,24 @@ inline void for_tables(const thc_tensors* t, Grid grid, uint32_t flat_bytes, uin
     launch(tab, units);
     k = units = 0;
   };
-  auto add = [&](void* ptr, uint64_t numel, uint32_t type) {
-    // a launch's units are numbered in 32 bits; 2^40 elements are 2^27 units, and a tensor adds at most one
-    if (k == TABLE) flush();
+  auto part = [&](void* ptr, uint64_t numel, uint32_t type) {
     const uint32_t size = grid == Grid::FLAT ? flat_bytes : type_bytes(type);
     const uint64_t addr = grid == Grid::FLAT ? at * size : reinterpret_cast<uintptr_t>(ptr);
+    const uint32_t own = (uint32_t)((addr % LINE + numel * size + (1u << log_unit) - 1) >> log_unit);
+    if (k == TABLE || units + own > MOST_UNITS) flush();
     tab.ptr[k] = ptr;
     tab.at[k] = at | (uint64_t)type << AT_BITS;
     tab.unit[k] = units;
-    units += (uint32_t)((addr % LINE / size + numel + UNIT - 1) >> LOG_UNIT);
+    units += own;
     at += numel;
     ++k;
+  };
+  auto add = [&](void* ptr, uint64_t numel, uint32_t type) {
+    for (; numel > MOST_NUMEL; numel -= MOST_NUMEL) {
+      part(ptr, MOST_NUMEL, type);
+      if (ptr) ptr = static_cast<char*>(ptr) + MOST_NUMEL * type_bytes(type);
+    }
+    part(ptr, numel, type);
   };
   void* run = nullptr;
   uint64_t len = 0;

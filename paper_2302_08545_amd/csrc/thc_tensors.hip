@@ -20,50 +20,106 @@ int check_norm(const thc_tensors* t, int kind, float max_norm, const float* norm
   return THC_OK;
 }
 
+// launch(arguments) with the table in the smaller form that holds it
+template <template <class> class Args, class Table, class Fill, class Launch>
+void with_table(const Table& tab, Fill&& fill, Launch&& launch) {
+  if (tab.count <= SHORT_TABLE) {
+    Args<TensorTable<SHORT_TABLE>> a;
+    fill(a);
+    shorten(tab, &a.tab);
+    launch(a);
+  } else {
+    Args<TensorTable<TABLE>> a;
+    fill(a);
+    a.tab = tab;
+    launch(a);
+  }
+}
+
 // the partials of all launches; returns their number
 template <int KIND>
-uint32_t run_partials(const thc_tensors* t, double* partials, hipStream_t s) {
-  uint32_t written = 0;
-  NormArgs a;
-  a.partials = partials;
-  for_tables(t, Grid::TENSOR, 0, 0, [&](const TensorTable& tab, uint32_t units) {
-    a.tab = tab;
-    a.units = units;
-    a.before = written;
-    const uint32_t groups = units < NORM_PARTIALS ? units : NORM_PARTIALS;
-    k_norm<KIND><<<dim3(groups), dim3(TNT), 0, s>>>(a);
+uint32_t run_partials(const thc_tensors* t, uint64_t bytes, bool in_place, double* partials, hipStream_t s) {
+  uint32_t written = 0, keep = (uint32_t)(norm_keeps(bytes, in_place) >> LOG_NORM_UNIT);
+  for_tables(t, Grid::TENSOR, 0, 0, LOG_NORM_UNIT, [&](const TensorTable<TABLE>& tab, uint32_t units) {
+    const uint32_t groups = units < NORM_PARTIALS ? units : NORM_PARTIALS, kept = keep < units ? keep : units;
+    with_table<NormArgs>(
+        tab,
+        [&](auto& a) {
+          a.partials = partials;
+          a.units = units;
+          a.keep = kept;
+          a.before = written;
+        },
+        [&](const auto& a) { k_norm<KIND><<<dim3(groups), dim3(TNT), 0, s>>>(a); });
+    keep -= kept;
     written = groups > written ? groups : written;
   });
   return written;
 }
 
 template <int KIND>
-int run_norm(const thc_tensors* t, NormOut o, double* partials, hipStream_t s) {
-  o.count = run_partials<KIND>(t, partials, s);
-  o.partials = partials;
-  k_norm_final<KIND><<<dim3(1), dim3(FINAL_NT), 0, s>>>(o);
-  return check_launch();
+void run_final(const FinalArgs& f, hipStream_t s) {
+  if (f.count <= 1024) k_norm_final<KIND, 256, 4><<<dim3(1), dim3(256), 0, s>>>(f);
+  else k_norm_final<KIND, FINAL_NT, NORM_PARTIALS / FINAL_NT><<<dim3(1), dim3(FINAL_NT), 0, s>>>(f);
+}
+
+// whether the list goes through one launch of one workgroup; if so, that is done
+template <int KIND>
+bool run_one(const thc_tensors* t, uint64_t bytes, bool in_place, NormOut o, hipStream_t s) {
+  if (bytes > ONE_MOST_UNITS << LOG_WAVE_UNIT || t->count > SHORT_TABLE) return false;
+  OneArgs a;
+  a.out = o;
+  a.units = a.tab.count = 0;
+  for_tables(t, Grid::TENSOR, 0, 0, LOG_WAVE_UNIT, [&](const TensorTable<TABLE>& tab, uint32_t units) {
+    shorten(tab, &a.tab);
+    a.units = units;
+  });
+  if (a.units > ONE_MOST_UNITS) return false;
+  if (in_place) k_norm_one<KIND, true><<<dim3(1), dim3(ONE_NT), 0, s>>>(a);
+  else k_norm_one<KIND, false><<<dim3(1), dim3(ONE_NT), 0, s>>>(a);
+  return true;
+}
+
+template <class Launch>
+void run_moves(const thc_tensors* t, Grid grid, uint32_t flat_bytes, uint64_t zeros, void* flat, const float* scale, Launch&& launch) {
+  for_tables(t, grid, flat_bytes, zeros, LOG_MOVE_UNIT, [&](const TensorTable<TABLE>& tab, uint32_t units) {
+    with_table<MoveArgs>(
+        tab,
+        [&](auto& a) {
+          a.flat = flat;
+          a.scale = scale;
+        },
+        [&](const auto& a) { launch(a, dim3(units)); });
+  });
 }
 
 template <int KIND>
-int run_clip(const thc_tensors* t, NormOut o, double* partials, hipStream_t s) {
-  o.count = run_partials<KIND>(t, partials, s);
-  o.partials = partials;
-  if (!o.count) {
-    k_norm_final<KIND><<<dim3(1), dim3(FINAL_NT), 0, s>>>(o);
-    return check_launch();
+void run_norm(const thc_tensors* t, NormOut o, double* partials, hipStream_t s) {
+  const uint64_t bytes = list_bytes(t);
+  if (run_one<KIND>(t, bytes, false, o, s)) return;
+  run_final<KIND>(FinalArgs{o, partials, run_partials<KIND>(t, bytes, false, partials, s)}, s);
+}
+
+template <int KIND>
+void run_clip(const thc_tensors* t, NormOut o, double* partials, hipStream_t s) {
+  const uint64_t bytes = list_bytes(t);
+  if (run_one<KIND>(t, bytes, true, o, s)) return;
+  const uint32_t count = run_partials<KIND>(t, bytes, true, partials, s);
+  if (count <= FUSED_PARTIALS) {
+    for_tables(t, Grid::TENSOR, 0, 0, LOG_MOVE_UNIT, [&](const TensorTable<TABLE>& tab, uint32_t units) {
+      with_table<FinishArgs>(
+          tab,
+          [&](auto& a) {
+            a.out = o;
+            a.partials = partials;
+            a.count = count;
+          },
+          [&](const auto& a) { k_finish_scale<KIND><<<dim3(units), dim3(TNT), 0, s>>>(a); });
+    });
+    return;
   }
-  ClipArgs a;
-  a.out = o;
-  a.first = 1;
-  for_tables(t, Grid::TENSOR, 0, 0, [&](const TensorTable& tab, uint32_t units) {
-    a.tab = tab;
-    a.units = units;
-    const uint32_t groups = units < NORM_PARTIALS ? units : NORM_PARTIALS;
-    k_clip<KIND><<<dim3(groups), dim3(TNT), 0, s>>>(a);
-    a.first = 0;
-  });
-  return check_launch();
+  run_final<KIND>(FinalArgs{o, partials, count}, s);
+  run_moves(t, Grid::TENSOR, 0, 0, nullptr, o.scale, [&](const auto& a, dim3 grid) { k_scale<<<grid, dim3(TNT), 0, s>>>(a); });
 }
 
 int check_flat(const thc_params* p, const thc_tensors* t, const void* flat, uint32_t flat_bytes, const float* scale,
@@ -82,17 +138,19 @@ extern "C" {
 
 int thc_norm_workspace_bytes(size_t* bytes_out) {
   if (!bytes_out) return THC_EINVAL;
-  *bytes_out = NORM_PARTIALS * sizeof(double);
+  *bytes_out = NORM_PARTIALS * sizeof(double) + 16;   // partials, and the factor where the caller keeps none
   return THC_OK;
 }
 
 int thc_grad_norm(const thc_tensors* t, int kind, float max_norm, float* norm_out, float* scale_out, void* ws, void* stream) {
   const int rc = check_norm(t, kind, max_norm, norm_out, scale_out, ws);
   if (rc) return rc;
-  const NormOut o{norm_out, scale_out, max_norm, 0, nullptr};
+  const NormOut o{norm_out, scale_out, max_norm};
   double* const partials = static_cast<double*>(ws);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  return kind == THC_NORM_L2 ? run_norm<THC_NORM_L2>(t, o, partials, s) : run_norm<THC_NORM_MAX>(t, o, partials, s);
+  if (kind == THC_NORM_L2) run_norm<THC_NORM_L2>(t, o, partials, s);
+  else run_norm<THC_NORM_MAX>(t, o, partials, s);
+  return check_launch();
 }
 
 int thc_grad_clip(const thc_tensors* t, int kind, float max_norm, float* norm_out, float* scale_out, void* ws, void* stream) {
@@ -100,10 +158,13 @@ int thc_grad_clip(const thc_tensors* t, int kind, float max_norm, float* norm_ou
   if (rc) return rc;
   rc = check_overlap(t, true, nullptr, 0);
   if (rc) return rc;
-  const NormOut o{norm_out, scale_out, max_norm, 0, nullptr};
-  double* const partials = static_cast<double*>(ws);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  return kind == THC_NORM_L2 ? run_clip<THC_NORM_L2>(t, o, partials, s) : run_clip<THC_NORM_MAX>(t, o, partials, s);
+  double* const partials = static_cast<double*>(ws);
+  float* const scale = scale_out ? scale_out : reinterpret_cast<float*>(partials + NORM_PARTIALS);
+  const NormOut o{norm_out, scale, max_norm};
+  if (kind == THC_NORM_L2) run_clip<THC_NORM_L2>(t, o, partials, s);
+  else run_clip<THC_NORM_MAX>(t, o, partials, s);
+  return check_launch();
 }
 
 int thc_gather(const thc_params* p, const thc_tensors* t, const float* scale, void* grad_out, void* stream) {
@@ -112,15 +173,9 @@ int thc_gather(const thc_params* p, const thc_tensors* t, const float* scale, vo
   const int rc = check_flat(p, t, grad_out, bytes, scale, false, &total);
   if (rc) return rc;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  GatherArgs a;
-  a.flat = grad_out;
-  a.scale = scale;
-  for_tables(t, Grid::FLAT, bytes, p->d - total, [&](const TensorTable& tab, uint32_t units) {
-    a.tab = tab;
-    a.units = units;
-    const dim3 grid(units < NORM_PARTIALS ? units : NORM_PARTIALS), blk(TNT);
-    if (bytes == 2) k_gather<Bf16><<<grid, blk, 0, s>>>(a);
-    else k_gather<float><<<grid, blk, 0, s>>>(a);
+  run_moves(t, Grid::FLAT, bytes, p->d - total, grad_out, scale, [&](const auto& a, dim3 grid) {
+    if (bytes == 2) k_gather<Bf16><<<grid, dim3(TNT), 0, s>>>(a);
+    else k_gather<float><<<grid, dim3(TNT), 0, s>>>(a);
   });
   return check_launch();
 }
@@ -130,14 +185,8 @@ int thc_scatter(const thc_params* p, const float* flat, const float* scale, cons
   const int rc = check_flat(p, t, flat, 4, scale, true, &total);
   if (rc) return rc;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  ScatterArgs a;
-  a.flat = flat;
-  a.scale = scale;
-  for_tables(t, Grid::TENSOR, 0, 0, [&](const TensorTable& tab, uint32_t units) {
-    a.tab = tab;
-    a.units = units;
-    k_scatter<<<dim3(units < NORM_PARTIALS ? units : NORM_PARTIALS), dim3(TNT), 0, s>>>(a);
-  });
+  run_moves(t, Grid::TENSOR, 0, 0, const_cast<float*>(flat), scale,
+            [&](const auto& a, dim3 grid) { k_scatter<<<grid, dim3(TNT), 0, s>>>(a); });
   return check_launch();
 }
 

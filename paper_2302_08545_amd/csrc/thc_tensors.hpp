@@ -11,9 +11,9 @@
 
 namespace thc {
 
-constexpr int TNT = 256;              // threads per workgroup
-constexpr uint32_t NORM_PARTIALS = 2048;   // most workgroups of a norm launch: one partial each
-constexpr int FINAL_NT = 1024;
+constexpr int TNT = 256;                   // threads per workgroup
+constexpr uint32_t NORM_PARTIALS = 8192;   // most workgroups of a norm launch: one partial each
+constexpr int FINAL_NT = 1024, ONE_NT = 1024;
 
 struct Bf16 { uint16_t bits; };
 struct F16 { _Float16 v; };
@@ -28,28 +28,51 @@ template <> __device__ __forceinline__ F16 narrow<F16>(float x) {
   return F16{(_Float16)x};
 }
 
-// N consecutive elements, aligned as one of them is: one access of up to 16 bytes (the GPU takes global accesses of any alignment)
 template <class T, int N>
-struct __attribute__((packed, aligned(sizeof(T)))) Pack { T x[N]; };
+struct Pack { T x[N]; };
+
+template <int WORDS, int ALIGN> struct Words;
+template <> struct Words<2, 2> { typedef uint32_t type __attribute__((ext_vector_type(2), aligned(2))); };
+template <> struct Words<4, 2> { typedef uint32_t type __attribute__((ext_vector_type(4), aligned(2))); };
+template <> struct Words<4, 4> { typedef uint32_t type __attribute__((ext_vector_type(4), aligned(4))); };
+
+// N consecutive elements, non-temporal, aligned as one of them is: the GPU takes global accesses of any alignment
+template <class T, int N>
+__device__ __forceinline__ Pack<T, N> load_pack(const T* p) {
+  using U = typename Words<sizeof(T) * N / 4, sizeof(T)>::type;
+  const U v = __builtin_nontemporal_load(reinterpret_cast<const U*>(p));
+  return __builtin_bit_cast(Pack<T, N>, v);
+}
+
+// Non-temporal, aligned to its size.  Plain stores would leave the lines to whoever reads them next, but they cost the call more: gather
+// of 128 MB 45.1 -> 48.7 us, with the norm before it 60.6 -> 77.8, scatter of 128 MB 43.3 -> 48.3, scaling in place 66.2 -> 86.8.  Together
+// with the next reading, us plain / non-temporal: norm, gather and compress 32 MB 46.2 / 46.9, 128 MB 138 / 142, 256 MB 266 / 262, bf16
+// 128 MB 179 / 178; decompress, scatter and an addition to every tensor 32 MB 54.7 / 55.8, 128 MB 166 / 172, 512 MB 656 / 649; scaling in
+// place and the addition 64 MB 58.0 / 58.0.
+template <class T, int N>
+__device__ __forceinline__ void store_pack(T* p, const Pack<T, N>& v) {
+  typedef uint32_t U __attribute__((ext_vector_type(sizeof(T) * N / 4)));
+  __builtin_nontemporal_store(__builtin_bit_cast(U, v), reinterpret_cast<U*>(p));
+}
 
 // The tensor that a unit belongs to, and the unit's place in it.
 struct Piece {
   char* ptr;
   uint64_t at;      // of the tensor's first element in the flat vector
-  uint64_t numel;
-  int64_t lo;       // the unit's first element, counted from the tensor's: negative where the grid starts before it
+  int64_t len;      // of the tensor, in bytes of the memory that the grid goes by
+  int64_t lo;       // the unit's first byte there, counted from the tensor's: negative where the grid starts before it
   uint32_t type;
 };
 
 // Each wave counts the tensors that start at or before the unit, 64 at a time.
-template <Grid GRID, uint32_t FLAT_BYTES>
-__device__ __forceinline__ Piece locate(const TensorTable& tab, uint32_t u) {
+template <uint32_t LOG_UNIT, Grid GRID, uint32_t FLAT_BYTES, class Table>
+__device__ __forceinline__ Piece locate(const Table& tab, uint32_t u) {
   const uint32_t lane = threadIdx.x & 63u;
   uint32_t n = 0;
 #pragma unroll
-  for (uint32_t k = 0; k < TABLE; k += 64) {
-    const bool before = k + lane < tab.count && tab.unit[k + lane] <= u;
-    n += (uint32_t)__popcll(__ballot(before));
+  for (uint32_t k = 0; k < Table::SIZE; k += 64) {
+    const uint32_t unit = tab.unit[k + lane];    // all at once: no condition before the load
+    n += (uint32_t)__popcll(__ballot((k + lane < tab.count) & (unit <= u)));
   }
   const uint32_t i = __builtin_amdgcn_readfirstlane(n - 1u);
   Piece p;
@@ -57,11 +80,30 @@ __device__ __forceinline__ Piece locate(const TensorTable& tab, uint32_t u) {
   p.ptr = static_cast<char*>(tab.ptr[i]);
   p.at = at & AT_MASK;
   p.type = (uint32_t)(at >> AT_BITS);
-  p.numel = (tab.at[i + 1] & AT_MASK) - p.at;
   const uint32_t size = GRID == Grid::FLAT ? FLAT_BYTES : p.type == TYPE_F32 ? 4 : 2;
+  p.len = (int64_t)(((tab.at[i + 1] & AT_MASK) - p.at) * size);
   const uint64_t addr = GRID == Grid::FLAT ? p.at * size : reinterpret_cast<uintptr_t>(p.ptr);
-  p.lo = ((int64_t)(u - tab.unit[i]) << LOG_UNIT) - (int64_t)(addr % LINE / size);
+  p.lo = (int64_t)((uint64_t)(u - tab.unit[i]) << LOG_UNIT) - (int64_t)(addr % LINE);
   return p;
+}
+
+// Units are cut into slots of SLOT bytes that lie on the grid.  The elements in front of a tensor's first whole slot and behind its
+// last one are taken one to a thread: the offset of this thread's, in bytes, or -1.
+template <uint32_t LOG_UNIT, int N, int SLOT, int SIZE>
+__device__ __forceinline__ int64_t edge(const Piece& p) {
+  constexpr int E = SLOT / SIZE;
+  static_assert(2 * E <= N);
+  const int t = (int)(threadIdx.x % N);
+  const int64_t first = p.lo < 0 ? p.lo & (SLOT - 1) : 0;          // where the first whole slot starts
+  const int64_t last = p.len - ((p.len - p.lo) & (SLOT - 1));      // where the last one ends
+  if (t < E) return p.lo < 0 && t * SIZE < first && t * SIZE < p.len ? t * SIZE : -1;
+  const int64_t j = last + (t - E) * SIZE;
+  return t < 2 * E && last >= first && last - p.lo < (1 << LOG_UNIT) && j < p.len ? j : -1;
+}
+__device__ __forceinline__ bool whole(const Piece& p, int64_t bytes) { return p.lo >= 0 && p.lo + bytes <= p.len; }
+template <int SLOT>
+__device__ __forceinline__ bool whole_slot(const Piece& p, uint32_t at) {
+  return p.lo + at >= 0 && p.lo + at + SLOT <= p.len;
 }
 
 // ---- norm ---------------------------------------------------------------------------------------------------------
@@ -106,181 +148,247 @@ __device__ __forceinline__ double group_join(double v) {
   return v;
 }
 
-template <int KIND, class T>
-__device__ __forceinline__ void norm_unit(const Piece& p, Acc<KIND>& acc) {
-  constexpr int V = 16 / sizeof(T), S = UNIT / V / TNT;
-  const T* const x = reinterpret_cast<const T*>(p.ptr) + p.lo;
-  const uint32_t t = threadIdx.x * V;
-  if (p.lo >= 0 && (uint64_t)p.lo + UNIT <= p.numel) {
-    Pack<T, V> v[S];
+template <class T, int S, class A>
+__device__ __forceinline__ void add_words(const uint4 (&v)[S], uint32_t one, A& acc) {
+  acc.add(widen(__builtin_bit_cast(Pack<T, 4 / sizeof(T)>, one).x[0]));
 #pragma unroll
-    for (int k = 0; k < S; ++k) v[k] = *reinterpret_cast<const Pack<T, V>*>(x + (t + k * TNT * V));
-#pragma unroll
-    for (int k = 0; k < S; ++k)
-#pragma unroll
-      for (int e = 0; e < V; ++e) acc.add(widen(v[k].x[e]));
-    return;
-  }
-#pragma unroll 1
   for (int k = 0; k < S; ++k) {
-    const int64_t j = p.lo + t + k * TNT * V;
-    if (j >= 0 && (uint64_t)j + V <= p.numel) {
-      const Pack<T, V> v = *reinterpret_cast<const Pack<T, V>*>(x + (t + k * TNT * V));
+    const auto x = __builtin_bit_cast(Pack<T, 16 / sizeof(T)>, v[k]);
 #pragma unroll
-      for (int e = 0; e < V; ++e) acc.add(widen(v.x[e]));
-    } else {
-#pragma unroll 1
-      for (int e = 0; e < V; ++e)
-        if (j + e >= 0 && (uint64_t)(j + e) < p.numel) acc.add(widen(x[t + k * TNT * V + e]));
-    }
+    for (int e = 0; e < 16 / (int)sizeof(T); ++e) acc.add(widen(x.x[e]));
+    __builtin_amdgcn_sched_barrier(0);   // 16 bytes after the other: all of them widened at once do not fit the registers
   }
 }
 
+// One unit, by N threads: its words are read the same way whatever they hold.
+template <uint32_t LOG_UNIT, int N, class A>
+__device__ __forceinline__ void norm_unit(const Piece& p, bool keep, A& acc) {
+  constexpr int S = (1 << LOG_UNIT) / 16 / N;
+  const char* const x = p.ptr + p.lo;
+  uint32_t t = threadIdx.x % N * 16;
+  asm("" : "+v"(t));   // offsets that are not worth a register between two units
+  uint4 v[S];
+  uint32_t one = 0;
+  if (!whole(p, 1 << LOG_UNIT)) {
+    const int64_t e = p.type == TYPE_F32 ? edge<LOG_UNIT, N, 16, 4>(p) : edge<LOG_UNIT, N, 16, 2>(p);
+    if (e >= 0) one = p.type == TYPE_F32 ? *reinterpret_cast<const uint32_t*>(p.ptr + e) : *reinterpret_cast<const uint16_t*>(p.ptr + e);
+#pragma unroll
+    for (int k = 0; k < S; ++k) {
+      v[k] = make_uint4(0, 0, 0, 0);
+      if (whole_slot<16>(p, t + k * N * 16)) v[k] = load_u4<KEEP>(x + (t + k * N * 16));
+    }
+  } else if (keep) {
+#pragma unroll
+    for (int k = 0; k < S; ++k) v[k] = load_u4<KEEP>(x + (t + k * N * 16));
+  } else {
+#pragma unroll
+    for (int k = 0; k < S; ++k) v[k] = load_u4<STREAM>(x + (t + k * N * 16));
+  }
+  if (p.type == TYPE_F32) add_words<float>(v, one, acc);
+  else if (p.type == TYPE_BF16) add_words<Bf16>(v, one, acc);
+  else add_words<F16>(v, one, acc);
+}
+
+template <class Table>
 struct NormArgs {
   double* partials;
   uint32_t units;
+  uint32_t keep;        // units that the caches are to hold on to: the launch's first ones
   uint32_t before;      // partials that an earlier launch of the call has written: these are added to
-  TensorTable tab;
+  Table tab;
 };
-static_assert(sizeof(NormArgs) <= 4096, "kernel arguments");
+static_assert(sizeof(NormArgs<TensorTable<TABLE>>) <= 4096, "kernel arguments");
 
-template <int KIND>
-__global__ __launch_bounds__(TNT) void k_norm(const NormArgs a) {
+template <int KIND, class Table>
+__global__ __launch_bounds__(TNT, 7) void k_norm(const NormArgs<Table> a) {
   Acc<KIND> acc;
   for (uint32_t u = blockIdx.x; u < a.units; u += gridDim.x) {
-    const Piece p = locate<Grid::TENSOR, 0>(a.tab, u);
-    if (p.type == TYPE_F32) norm_unit<KIND, float>(p, acc);
-    else if (p.type == TYPE_BF16) norm_unit<KIND, Bf16>(p, acc);
-    else norm_unit<KIND, F16>(p, acc);
+    const Piece p = locate<LOG_NORM_UNIT, Grid::TENSOR, 0>(a.tab, u);
+    norm_unit<LOG_NORM_UNIT, TNT>(p, u < a.keep, acc);
   }
   const double v = group_join<KIND, TNT>(acc.get());
   if (threadIdx.x == 0) a.partials[blockIdx.x] = blockIdx.x < a.before ? Acc<KIND>::join(a.partials[blockIdx.x], v) : v;
-}
-
-// the norm and the factor that clips by it, from the partials
-template <int KIND, int N>
-__device__ __forceinline__ double norm_of(const double* partials, uint32_t count) {
-  double v = 0.0;
-  for (uint32_t i = threadIdx.x; i < count; i += N) v = Acc<KIND>::join(v, partials[i]);
-  v = group_join<KIND, N>(v);
-  return KIND == THC_NORM_L2 ? __builtin_sqrt(v) : v;
-}
-__device__ __forceinline__ float clip_factor(double norm, float max_norm) {
-  return norm <= (double)max_norm ? 1.f : (float)((double)max_norm / norm);
 }
 
 struct NormOut {
   float* norm;
   float* scale;         // or null
   float max_norm;
-  uint32_t count;       // partials
-  const double* partials;
 };
 
+// the factor that clips, from the sum of squares or the largest magnitude; one thread of the launch writes both
 template <int KIND>
-__global__ __launch_bounds__(FINAL_NT) void k_norm_final(const NormOut o) {
-  const double v = norm_of<KIND, FINAL_NT>(o.partials, o.count);
-  if (threadIdx.x == 0) {
-    *o.norm = (float)v;
-    if (o.scale) *o.scale = clip_factor(v, o.max_norm);
+__device__ __forceinline__ float finish(const NormOut& o, double v, bool writes) {
+  const double norm = KIND == THC_NORM_L2 ? __builtin_sqrt(v) : v;
+  const float c = norm <= (double)o.max_norm ? 1.f : (float)((double)o.max_norm / norm);
+  if (writes) {
+    *o.norm = (float)norm;
+    if (o.scale) *o.scale = c;
   }
+  return c;
+}
+
+struct FinalArgs {
+  NormOut out;
+  const double* partials;
+  uint32_t count;
+};
+
+// N threads take up to PER partials each
+template <int KIND, int N, int PER>
+__global__ __launch_bounds__(N) void k_norm_final(const FinalArgs a) {
+  double x[PER];
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const uint32_t i = threadIdx.x + k * N;
+    x[k] = i < a.count ? a.partials[i] : 0.0;
+  }
+  double v = x[0];
+#pragma unroll
+  for (int k = 1; k < PER; ++k) v = Acc<KIND>::join(v, x[k]);
+  finish<KIND>(a.out, group_join<KIND, N>(v), threadIdx.x == 0);
 }
 
 // ---- moves --------------------------------------------------------------------------------------------------------
-// dst[j] = round(src[j] * c) over one unit, whole 16-byte stores but at a tensor's ends
-template <class S, class D>
-__device__ __forceinline__ void move_unit(const S* src, D* dst, int64_t lo, uint64_t numel, float c) {
-  constexpr int V = 16 / sizeof(D), K = UNIT / V / TNT;
-  src += lo;
-  dst += lo;
-  const uint32_t t = threadIdx.x * V;
-  if (lo >= 0 && (uint64_t)lo + UNIT <= numel) {
-    Pack<S, V> v[K];
+// dst[j] = round(src[j] * c) over one unit of dst, by N threads: whole lines but at a tensor's ends
+template <uint32_t LOG_UNIT, int N, class S, class D>
+__device__ __forceinline__ void move_unit(const S* src, D* dst, const Piece& p, float c) {
+  constexpr int V = 16 / (sizeof(S) > sizeof(D) ? sizeof(S) : sizeof(D)), SLOT = V * sizeof(D), K = (1 << LOG_UNIT) / SLOT / N;
+  const S* const x = src + (p.lo >> (sizeof(D) / 2));            // a whole number of elements
+  D* const y = dst + (p.lo >> (sizeof(D) / 2));
+  const uint32_t t = threadIdx.x % N * V;
+  auto scaled = [&](const Pack<S, V>& v) {
+    Pack<D, V> o;
 #pragma unroll
-    for (int k = 0; k < K; ++k) v[k] = *reinterpret_cast<const Pack<S, V>*>(src + (t + k * TNT * V));
+    for (int e = 0; e < V; ++e) o.x[e] = narrow<D>(widen(v.x[e]) * c);
+    return o;
+  };
+  Pack<S, V> v[K];
+  if (whole(p, 1 << LOG_UNIT)) {
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      Pack<D, V> o;
+    for (int k = 0; k < K; ++k) v[k] = load_pack<S, V>(x + (t + k * N * V));
 #pragma unroll
-      for (int e = 0; e < V; ++e) o.x[e] = narrow<D>(widen(v[k].x[e]) * c);
-      *reinterpret_cast<Pack<D, V>*>(__builtin_assume_aligned(dst + (t + k * TNT * V), 16)) = o;
-    }
+    for (int k = 0; k < K; ++k) store_pack<D, V>(y + (t + k * N * V), scaled(v[k]));
     return;
   }
-#pragma unroll 1
+  const int64_t at = edge<LOG_UNIT, N, SLOT, sizeof(D)>(p);
+  S one{};
+  if (at >= 0) one = src[at >> (sizeof(D) / 2)];
+#pragma unroll
+  for (int k = 0; k < K; ++k)
+    if (whole_slot<SLOT>(p, (t + k * N * V) * sizeof(D))) v[k] = load_pack<S, V>(x + (t + k * N * V));
+  if (at >= 0) dst[at >> (sizeof(D) / 2)] = narrow<D>(widen(one) * c);
+#pragma unroll
+  for (int k = 0; k < K; ++k)
+    if (whole_slot<SLOT>(p, (t + k * N * V) * sizeof(D))) store_pack<D, V>(y + (t + k * N * V), scaled(v[k]));
+}
+
+// zeros, likewise
+template <class D>
+__device__ __forceinline__ void zero_unit(D* dst, const Piece& p) {
+  constexpr int V = 16 / sizeof(D), K = (1 << LOG_MOVE_UNIT) / 16 / TNT;
+  const int64_t e = edge<LOG_MOVE_UNIT, TNT, 16, sizeof(D)>(p);
+  if (e >= 0) dst[e >> (sizeof(D) / 2)] = D{};
+#pragma unroll
   for (int k = 0; k < K; ++k) {
-    const uint32_t i = t + k * TNT * V;
-    const int64_t j = lo + i;
-#pragma unroll 1
-    for (int e = 0; e < V; ++e)
-      if (j + e >= 0 && (uint64_t)(j + e) < numel) dst[i + e] = narrow<D>(widen(src[i + e]) * c);
+    const uint32_t i = (threadIdx.x + k * TNT) * V;
+    if (whole_slot<16>(p, i * sizeof(D))) store_pack<D, V>(dst + ((p.lo >> (sizeof(D) / 2)) + i), Pack<D, V>{});
   }
 }
 
-struct ClipArgs {
-  NormOut out;
-  uint32_t units;
-  uint32_t first;       // 1 in the launch that writes the norm
-  TensorTable tab;
-};
-static_assert(sizeof(ClipArgs) <= 4096, "kernel arguments");
-
-template <int KIND>
-__global__ __launch_bounds__(TNT) void k_clip(const ClipArgs a) {
-  const double v = norm_of<KIND, TNT>(a.out.partials, a.out.count);
-  const float c = clip_factor(v, a.out.max_norm);
-  if (a.first && blockIdx.x == 0 && threadIdx.x == 0) {
-    *a.out.norm = (float)v;
-    if (a.out.scale) *a.out.scale = c;
-  }
-  if (c == 1.f) return;
-  for (uint32_t u = blockIdx.x; u < a.units; u += gridDim.x) {
-    const Piece p = locate<Grid::TENSOR, 0>(a.tab, u);
-    if (p.type == TYPE_F32) move_unit(reinterpret_cast<const float*>(p.ptr), reinterpret_cast<float*>(p.ptr), p.lo, p.numel, c);
-    else if (p.type == TYPE_BF16) move_unit(reinterpret_cast<const Bf16*>(p.ptr), reinterpret_cast<Bf16*>(p.ptr), p.lo, p.numel, c);
-    else move_unit(reinterpret_cast<const F16*>(p.ptr), reinterpret_cast<F16*>(p.ptr), p.lo, p.numel, c);
-  }
+template <uint32_t LOG_UNIT, int N>
+__device__ __forceinline__ void scale_piece(const Piece& p, float c) {
+  if (p.type == TYPE_F32) move_unit<LOG_UNIT, N>(reinterpret_cast<const float*>(p.ptr), reinterpret_cast<float*>(p.ptr), p, c);
+  else if (p.type == TYPE_BF16) move_unit<LOG_UNIT, N>(reinterpret_cast<const Bf16*>(p.ptr), reinterpret_cast<Bf16*>(p.ptr), p, c);
+  else move_unit<LOG_UNIT, N>(reinterpret_cast<const F16*>(p.ptr), reinterpret_cast<F16*>(p.ptr), p, c);
 }
 
-struct GatherArgs {
+// flat: the vector, or null where the tensors are scaled in place
+template <class Table>
+struct MoveArgs {
   void* flat;
   const float* scale;   // or null
-  uint32_t units;
-  TensorTable tab;
+  Table tab;
 };
-static_assert(sizeof(GatherArgs) <= 4096, "kernel arguments");
+static_assert(sizeof(MoveArgs<TensorTable<TABLE>>) <= 4096, "kernel arguments");
 
-template <class D>
-__global__ __launch_bounds__(TNT) void k_gather(const GatherArgs a) {
-  const float c = a.scale ? *a.scale : 1.f;
-  for (uint32_t u = blockIdx.x; u < a.units; u += gridDim.x) {
-    const Piece p = locate<Grid::FLAT, sizeof(D)>(a.tab, u);
-    D* const dst = static_cast<D*>(a.flat) + p.at;
-    if (p.type == TYPE_F32) move_unit(reinterpret_cast<const float*>(p.ptr), dst, p.lo, p.numel, c);
-    else if (p.type == TYPE_BF16) move_unit(reinterpret_cast<const Bf16*>(p.ptr), dst, p.lo, p.numel, c);
-    else if (p.type == TYPE_F16) move_unit(reinterpret_cast<const F16*>(p.ptr), dst, p.lo, p.numel, c);
-    else
-      for (uint32_t i = threadIdx.x; i < UNIT; i += TNT)
-        if (p.lo + i >= 0 && (uint64_t)(p.lo + i) < p.numel) dst[p.lo + i] = narrow<D>(0.f);
-  }
+// The same from up to FUSED_PARTIALS partials, which each wave adds up by itself: the launch of k_norm_final is saved.
+constexpr uint32_t FUSED_PARTIALS = 384;
+
+template <class Table>
+struct FinishArgs {
+  NormOut out;
+  const double* partials;
+  uint32_t count;
+  Table tab;
+};
+
+template <int KIND, class Table>
+__global__ __launch_bounds__(TNT, 8) void k_finish_scale(const FinishArgs<Table> a) {
+  const uint32_t lane = threadIdx.x & 63u;
+  double x[FUSED_PARTIALS / 64];
+#pragma unroll
+  for (uint32_t k = 0; k < FUSED_PARTIALS / 64; ++k) x[k] = lane + 64 * k < a.count ? a.partials[lane + 64 * k] : 0.0;
+  double v = x[0];
+#pragma unroll
+  for (uint32_t k = 1; k < FUSED_PARTIALS / 64; ++k) v = Acc<KIND>::join(v, x[k]);
+  const float c = finish<KIND>(a.out, wave_join<KIND>(v), blockIdx.x == 0 && threadIdx.x == 0);
+  if (c == 1.f) return;
+  scale_piece<LOG_MOVE_UNIT, TNT>(locate<LOG_MOVE_UNIT, Grid::TENSOR, 0>(a.tab, blockIdx.x), c);
 }
 
-struct ScatterArgs {
-  const float* flat;
-  const float* scale;   // or null
-  uint32_t units;
-  TensorTable tab;
-};
-static_assert(sizeof(ScatterArgs) <= 4096, "kernel arguments");
+template <class Table>
+__global__ __launch_bounds__(TNT, 8) void k_scale(const MoveArgs<Table> a) {
+  const float c = *a.scale;
+  if (c == 1.f) return;
+  scale_piece<LOG_MOVE_UNIT, TNT>(locate<LOG_MOVE_UNIT, Grid::TENSOR, 0>(a.tab, blockIdx.x), c);
+}
 
-__global__ __launch_bounds__(TNT) void k_scatter(const ScatterArgs a) {
+template <class D, class Table>
+__global__ __launch_bounds__(TNT, 8) void k_gather(const MoveArgs<Table> a) {
   const float c = a.scale ? *a.scale : 1.f;
-  for (uint32_t u = blockIdx.x; u < a.units; u += gridDim.x) {
-    const Piece p = locate<Grid::TENSOR, 0>(a.tab, u);
-    const float* const src = a.flat + p.at;
-    if (p.type == TYPE_F32) move_unit(src, reinterpret_cast<float*>(p.ptr), p.lo, p.numel, c);
-    else if (p.type == TYPE_BF16) move_unit(src, reinterpret_cast<Bf16*>(p.ptr), p.lo, p.numel, c);
-    else move_unit(src, reinterpret_cast<F16*>(p.ptr), p.lo, p.numel, c);
+  const Piece p = locate<LOG_MOVE_UNIT, Grid::FLAT, sizeof(D)>(a.tab, blockIdx.x);
+  D* const dst = static_cast<D*>(a.flat) + p.at;
+  if (p.type == TYPE_F32) move_unit<LOG_MOVE_UNIT, TNT>(reinterpret_cast<const float*>(p.ptr), dst, p, c);
+  else if (p.type == TYPE_BF16) move_unit<LOG_MOVE_UNIT, TNT>(reinterpret_cast<const Bf16*>(p.ptr), dst, p, c);
+  else if (p.type == TYPE_F16) move_unit<LOG_MOVE_UNIT, TNT>(reinterpret_cast<const F16*>(p.ptr), dst, p, c);
+  else zero_unit(dst, p);
+}
+
+template <class Table>
+__global__ __launch_bounds__(TNT, 8) void k_scatter(const MoveArgs<Table> a) {
+  const float c = a.scale ? *a.scale : 1.f;
+  const Piece p = locate<LOG_MOVE_UNIT, Grid::TENSOR, 0>(a.tab, blockIdx.x);
+  const float* const src = static_cast<const float*>(a.flat) + p.at;
+  if (p.type == TYPE_F32) move_unit<LOG_MOVE_UNIT, TNT>(src, reinterpret_cast<float*>(p.ptr), p, c);
+  else if (p.type == TYPE_BF16) move_unit<LOG_MOVE_UNIT, TNT>(src, reinterpret_cast<Bf16*>(p.ptr), p, c);
+  else move_unit<LOG_MOVE_UNIT, TNT>(src, reinterpret_cast<F16*>(p.ptr), p, c);
+}
+
+// ---- small lists ----------------------------------------------------------------------------------------------------
+// One workgroup, a unit to a wave, takes a list through the norm and, with SCALE, the scaling.  With up to two units a wave it is done
+// before two more launches would be.  us, this / the launches: binary32, 4 KB in one tensor 2.5 / 4.1 (with the scaling 2.4 / 5.7),
+// 64 KB in 8 3.1 / 4.7 (3.0 / 6.2), 128 KB in one 3.9 / 4.3 (3.8 / 5.9); bf16 128 KB 4.7 / 4.6 (4.8 / 6.2); three units a wave: 4 KB
+// in 48 tensors 5.5 / 4.8 (5.4 / 6.3), bf16 6.7 / 5.1 (7.2 / 6.7); four: 256 KB 5.3 / 4.5 (5.2 / 5.9).
+constexpr uint32_t ONE_MOST_UNITS = 2 * ONE_NT / 64;
+
+struct OneArgs {
+  NormOut out;
+  uint32_t units;
+  TensorTable<SHORT_TABLE> tab;
+};
+
+template <int KIND, bool SCALE>
+__global__ __launch_bounds__(ONE_NT) void k_norm_one(const OneArgs a) {
+  const uint32_t wave = threadIdx.x >> 6;
+  Acc<KIND> acc;
+  for (uint32_t u = wave; u < a.units; u += ONE_NT / 64)
+    norm_unit<LOG_WAVE_UNIT, 64>(locate<LOG_WAVE_UNIT, Grid::TENSOR, 0>(a.tab, u), true, acc);
+  const float c = finish<KIND>(a.out, group_join<KIND, ONE_NT>(acc.get()), threadIdx.x == 0);   // behind a barrier: everything has been read
+  if constexpr (SCALE) {
+    if (c == 1.f) return;
+    for (uint32_t u = wave; u < a.units; u += ONE_NT / 64)
+      scale_piece<LOG_WAVE_UNIT, 64>(locate<LOG_WAVE_UNIT, Grid::TENSOR, 0>(a.tab, u), c);
   }
 }
 

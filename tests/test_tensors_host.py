@@ -141,6 +141,7 @@ def test_make_tensors_takes_runs_of_memory_only():
 def test_lists_of_another_device_than_the_current_one_are_refused(monkeypatch):
     t = api.make_tensors([_gpu(torch.zeros(4), at=1)])
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
     for call in (lambda: api.thc_grad_norm(t, 0, 1.0, 16, 16, 16), lambda: api.thc_grad_clip(t, 0, 1.0, 16, 16, 16),
                  lambda: api.thc_gather(_p(), t, None, 1 << 44), lambda: api.thc_scatter(_p(), 1 << 44, None, t)):
         with pytest.raises(ValueError, match="cuda:1"):
