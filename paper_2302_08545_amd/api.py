@@ -4,6 +4,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from array import array
 from typing import Optional, Sequence
 
 _LIB = None
@@ -199,20 +200,21 @@ def thc_uniform_decompress(p: thc_params, rnd: int, agg, rotate: bool, range_m, 
 
 
 # ---- a model's tensors -----------------------------------------------------------------------------
-_DTYPES = {}       # torch's types, filled on first use: importing this module does not import torch
+_TORCH = None      # torch, and its types' codes, on first use: importing this module does not import torch
+_DTYPES = {}
 
 
-def _dtypes():
-    if not _DTYPES:
+def _torch():
+    global _TORCH
+    if _TORCH is None:
         import torch
         _DTYPES.update({torch.float32: THC_DTYPE_F32, torch.bfloat16: THC_DTYPE_BF16, torch.float16: THC_DTYPE_F16})
-    return _DTYPES
+        _TORCH = torch
+    return _TORCH
 
 
 def _one_run(t) -> bool:
     """Whether a tensor's elements lie in one run of memory, whatever the order of its dimensions."""
-    if t.is_contiguous():
-        return True
     at = 1
     for stride, size in sorted((st, n) for st, n in zip(t.stride(), t.shape) if n != 1):
         if stride != at:
@@ -227,21 +229,27 @@ def make_tensors(tensors: Sequence) -> thc_tensors:
     Each tensor is taken in the order of its memory, so it has to be one run of memory: contiguous, or with its
     dimensions in another order (channels last, transposed).  The list holds the tensors and the addresses that they
     have now: keep it as long as they stay where they are, and make a new one when a gradient is replaced."""
-    import torch
-    ts, types = tuple(tensors), _dtypes()
-    n, device = len(ts), None
+    ts, n = tuple(tensors), 0
+    _torch()
+    try:                   # a training step may make a list of hundreds: each property of all of them in one go
+        n = len(ts)
+        types = array("I", [_DTYPES[t.dtype] for t in ts])
+        devices = {t.get_device() for t in ts}
+        data = array("Q", [t.data_ptr() for t in ts])
+        numel = array("Q", [t.numel() for t in ts])
+    except (AttributeError, KeyError, RuntimeError, TypeError):
+        devices = {-1}
+    if -1 in devices:
+        raise ValueError("make_tensors: takes dense float32, bfloat16 and float16 tensors on the GPU")
+    if len(devices) > 1:
+        raise ValueError("make_tensors: all tensors have to be on one device")
     for t in ts:
-        if not isinstance(t, torch.Tensor) or t.layout != torch.strided or not t.is_cuda or t.dtype not in types:
-            raise ValueError("make_tensors: takes float32, bfloat16 and float16 tensors on the GPU")
-        if device is not None and t.get_device() != device:
-            raise ValueError("make_tensors: all tensors have to be on one device")
-        device = t.get_device()
-        if not _one_run(t):
+        if not t.is_contiguous() and not _one_run(t):
             raise ValueError(f"make_tensors: a tensor of shape {tuple(t.shape)} with strides {tuple(t.stride())} is not one "
                              "run of memory")
-    out = thc_tensors(n, (C.c_void_p * n)(*[t.data_ptr() for t in ts]), (C.c_uint64 * n)(*[t.numel() for t in ts]),
-                      (C.c_uint32 * n)(*[types[t.dtype] for t in ts]))
-    out.tensors, out.device = ts, device
+    out = thc_tensors(n, (C.c_void_p * n).from_buffer(data), (C.c_uint64 * n).from_buffer(numel),
+                      (C.c_uint32 * n).from_buffer(types)) if n else thc_tensors()
+    out.tensors, out.device = ts, devices.pop() if n else None
     return out
 
 
@@ -249,27 +257,30 @@ def _list_and_stream(tensors, stream, where: str):
     """The list as the library takes it, and the stream's handle.  The current stream is the current device's: the tensors
     have to be there too."""
     t = tensors if type(tensors) is thc_tensors else make_tensors(tensors)
-    if stream is None:
-        if t.device is not None:
-            import torch
-            try:
-                current = torch._C._cuda_getDevice()
-            except AttributeError:
-                current = torch.cuda.current_device()
-            if current != t.device:
-                raise ValueError(f"{where}: the tensors are on cuda:{t.device}, the current device is cuda:{current}")
-        return t, _stream(None)
+    if stream is None and t.device is not None:
+        try:
+            current = _TORCH._C._cuda_getDevice()
+        except AttributeError:                   # a name of torch's own that a build may lack
+            current = _TORCH.cuda.current_device()
+        if current != t.device:
+            raise ValueError(f"{where}: the tensors are on cuda:{t.device}, the current device is cuda:{current}")
+        try:
+            return t, _TORCH._C._cuda_getCurrentRawStream(current)
+        except AttributeError:
+            pass
     return t, _stream(stream)
 
 
-def _buffer(b, name: str, where: str, count: int, dtype=None) -> Optional[int]:
-    """The address of a tensor on the GPU that has to hold `count` elements of a type (None: bytes) in one run; addresses as they are."""
-    if b is None or isinstance(b, int):
+def _buffer(b, name: str, where: str, count: int, dtype: Optional[int]) -> Optional[int]:
+    """The address of a tensor on the GPU that has to hold `count` elements of a type (None: bytes) in one run; addresses as
+    they are."""
+    if b is None or type(b) is int:
         return b
     if dtype is None:
-        ok = b.numel() * b.element_size() >= count
+        ok = b.nbytes >= count
     else:
-        ok = _dtypes().get(b.dtype) == dtype and b.numel() >= count
+        _torch()
+        ok = b.numel() >= count and _DTYPES.get(b.dtype) == dtype
     if not (ok and b.is_cuda and b.is_contiguous()):
         raise ValueError(f"{where}: {name} has to be a contiguous tensor on the GPU with room for {count} "
                          f"{'bytes' if dtype is None else 'values of its type'}")
@@ -291,7 +302,7 @@ def _norm_call(call, where: str, tensors, kind, max_norm, norm_out, scale_out, w
         _NORM_WS = thc_norm_workspace_bytes()
     t, stream = _list_and_stream(tensors, stream, where)
     rc = call(t, kind, max_norm, _buffer(norm_out, "norm_out", where, 1, THC_DTYPE_F32),
-              _buffer(scale_out, "scale_out", where, 1, THC_DTYPE_F32), _buffer(ws, "ws", where, _NORM_WS), stream)
+              _buffer(scale_out, "scale_out", where, 1, THC_DTYPE_F32), _buffer(ws, "ws", where, _NORM_WS, None), stream)
     if rc != 0:
         raise ThcError(rc, where)
 

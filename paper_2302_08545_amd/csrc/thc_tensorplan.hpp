@@ -23,27 +23,35 @@ constexpr uint32_t MOST_UNITS = 1u << 23;
 constexpr uint64_t MOST_NUMEL = 1ull << 33;
 static_assert((MOST_NUMEL * 4 >> LOG_MOVE_UNIT) < MOST_UNITS);
 
-// Tensors of one launch, passed by value (a captured graph keeps them): a kernel's arguments have to stay within 4 KB.  Short lists
-// travel in a table of their own: a third of the arguments to write and, per wave, of the places to look at.
-constexpr uint32_t TABLE = 192, SHORT_TABLE = 64;
-constexpr int AT_BITS = 40;
-constexpr uint64_t AT_MASK = (1ull << AT_BITS) - 1;
+// Tensors of one launch, passed by value (a captured graph keeps them): a kernel's arguments have to stay within 4 KB, which 16 bytes
+// a tensor let hold 244.  Short lists travel in a table of their own: a third of the arguments to write and, per wave, a quarter of
+// the places to look at.
+constexpr uint32_t TABLE = 244, SHORT_TABLE = 63;
+constexpr int PTR_BITS = 48, AT_BITS = 40;     // of a device address, and of a place in the flat vector
+constexpr uint64_t PTR_MASK = (1ull << PTR_BITS) - 1, AT_MASK = (1ull << AT_BITS) - 1;
 enum { TYPE_F32 = THC_DTYPE_F32, TYPE_BF16 = THC_DTYPE_BF16, TYPE_F16 = THC_DTYPE_F16, TYPE_ZEROS = 3 };
 
 template <uint32_t N>
 struct TensorTable {
-  static constexpr uint32_t SIZE = N;
-  void* ptr[N];
-  uint64_t at[N + 1];     // first element's place in the flat vector, and above AT_BITS the tensor's type
-  uint32_t unit[N + 1];   // first unit; behind the last tensor the number of units
-  uint32_t count;
+  static constexpr uint32_t SIZE = N, LANES = (N + 64) / 64;   // places that one of 64 lanes looks at
+  uint32_t unit[64 * LANES];   // each tensor's first unit; behind the last one no unit is as large
+  uint64_t ptr[N + 1];         // address; above PTR_BITS the upper 8 bits of the place in the flat vector, then the type
+  uint32_t at[N + 1];          // the lower 32 bits of the first element's place in the flat vector; behind the last tensor its end
+  void set(uint32_t k, const void* p, uint64_t place, uint32_t type, uint32_t first) {
+    unit[k] = first;
+    ptr[k] = (reinterpret_cast<uintptr_t>(p) & PTR_MASK) | (place >> 32) << PTR_BITS | (uint64_t)type << (PTR_BITS + 8);
+    at[k] = (uint32_t)place;
+  }
+  void end(uint32_t k, uint64_t place) {
+    set(k, nullptr, place, 0, ~0u);
+    std::fill(unit + k, unit + 64 * LANES, ~0u);
+  }
 };
 
-inline void shorten(const TensorTable<TABLE>& from, TensorTable<SHORT_TABLE>* to) {
-  std::copy(from.ptr, from.ptr + from.count, to->ptr);
-  std::copy(from.at, from.at + from.count + 1, to->at);
-  std::copy(from.unit, from.unit + from.count + 1, to->unit);
-  to->count = from.count;
+inline void shorten(const TensorTable<TABLE>& from, uint32_t count, TensorTable<SHORT_TABLE>* to) {
+  std::copy(from.unit, from.unit + 64, to->unit);
+  std::copy(from.ptr, from.ptr + count + 1, to->ptr);
+  std::copy(from.at, from.at + count + 1, to->at);
 }
 
 inline uint32_t type_bytes(uint32_t type) { return type == TYPE_F32 ? 4 : 2; }
@@ -54,7 +62,8 @@ inline int validate_tensors(const thc_tensors* t, uint64_t* total) {
   if (t->count && (!t->data || !t->numel || !t->dtype)) return THC_EINVAL;
   for (uint64_t i = 0; i < t->count; ++i) {
     if (t->dtype[i] > THC_DTYPE_F16 || t->numel[i] > AT_MASK) return THC_EINVAL;
-    if (t->numel[i] && (!t->data[i] || reinterpret_cast<uintptr_t>(t->data[i]) % type_bytes(t->dtype[i]))) return THC_EINVAL;
+    const uintptr_t a = reinterpret_cast<uintptr_t>(t->data[i]);
+    if (t->numel[i] && (!a || a >> PTR_BITS || a % type_bytes(t->dtype[i]))) return THC_EINVAL;
     *total += t->numel[i];
     if (*total > AT_MASK) return THC_EINVAL;
   }
@@ -113,34 +122,10 @@ inline int check_overlap(const thc_tensors* t, bool each_other, const void* flat
 // Which memory a call's units are aligned to.
 enum class Grid { TENSOR, FLAT };
 
-// The tables of a call, one after another: launch(table, units of the table).  Tensors without elements take no place, and one
-// that starts where the one before it ends, with the same type, is part of it.  `zeros`: that many zeros follow the last tensor
-// in the flat vector.  `flat_bytes`: bytes per element of the flat vector (Grid::FLAT).  `log_unit`: of a unit's bytes.
-template <class Launch>
-inline void for_tables(const thc_tensors* t, Grid grid, uint32_t flat_bytes, uint64_t zeros, uint32_t log_unit, Launch&& launch) {
-  TensorTable<TABLE> tab;
-  uint32_t k = 0, units = 0;
-  uint64_t at = 0;
-  auto flush = [&] {
-    if (!k) return;
-    tab.at[k] = at;
-    tab.unit[k] = units;
-    tab.count = k;
-    launch(tab, units);
-    k = units = 0;
-  };
-  auto part = [&](void* ptr, uint64_t numel, uint32_t type) {
-    const uint32_t size = grid == Grid::FLAT ? flat_bytes : type_bytes(type);
-    const uint64_t addr = grid == Grid::FLAT ? at * size : reinterpret_cast<uintptr_t>(ptr);
-    const uint32_t own = (uint32_t)((addr % LINE + numel * size + (1u << log_unit) - 1) >> log_unit);
-    if (k == TABLE || units + own > MOST_UNITS) flush();
-    tab.ptr[k] = ptr;
-    tab.at[k] = at | (uint64_t)type << AT_BITS;
-    tab.unit[k] = units;
-    units += own;
-    at += numel;
-    ++k;
-  };
+// The entries of a list: part(address, elements, type).  Tensors without elements take no place, and one that starts where the one
+// before it ends, with the same type, is part of it.  `zeros`: that many zeros follow the last tensor in the flat vector.
+template <class Part>
+inline void for_parts(const thc_tensors* t, uint64_t zeros, Part&& part) {
   auto add = [&](void* ptr, uint64_t numel, uint32_t type) {
     for (; numel > MOST_NUMEL; numel -= MOST_NUMEL) {
       part(ptr, MOST_NUMEL, type);
@@ -164,6 +149,34 @@ inline void for_tables(const thc_tensors* t, Grid grid, uint32_t flat_bytes, uin
   }
   if (len) add(run, len, type);
   if (zeros) add(nullptr, zeros, TYPE_ZEROS);
+}
+
+// The tables of a call, one after another: launch(table, its tensors, its units).  Longer lists are cut into as many tensors a launch: 391
+// tensors as 196 and 195, not 244 and 147.  `flat_bytes`: bytes per element of the flat vector (Grid::FLAT).  `log_unit`: of a unit's bytes.
+template <class Launch>
+inline void for_tables(const thc_tensors* t, Grid grid, uint32_t flat_bytes, uint64_t zeros, uint32_t log_unit, Launch&& launch) {
+  uint64_t entries = 0;
+  if (t->count >= TABLE) for_parts(t, zeros, [&](void*, uint64_t, uint32_t) { ++entries; });
+  const uint64_t launches = (entries + TABLE - 1) / TABLE;
+  const uint32_t most = launches ? (uint32_t)((entries + launches - 1) / launches) : TABLE;
+  TensorTable<TABLE> tab;
+  uint32_t k = 0, units = 0;
+  uint64_t at = 0;
+  auto flush = [&] {
+    if (!k) return;
+    tab.end(k, at);
+    launch(tab, k, units);
+    k = units = 0;
+  };
+  for_parts(t, zeros, [&](void* ptr, uint64_t numel, uint32_t type) {
+    const uint32_t size = grid == Grid::FLAT ? flat_bytes : type_bytes(type);
+    const uint64_t addr = grid == Grid::FLAT ? at * size : reinterpret_cast<uintptr_t>(ptr);
+    const uint32_t own = (uint32_t)((addr % LINE + numel * size + (1u << log_unit) - 1) >> log_unit);
+    if (k == most || units + own > MOST_UNITS) flush();
+    tab.set(k++, ptr, at, type, units);
+    units += own;
+    at += numel;
+  });
   flush();
 }
 

@@ -22,11 +22,11 @@ int check_norm(const thc_tensors* t, int kind, float max_norm, const float* norm
 
 // launch(arguments) with the table in the smaller form that holds it
 template <template <class> class Args, class Table, class Fill, class Launch>
-void with_table(const Table& tab, Fill&& fill, Launch&& launch) {
-  if (tab.count <= SHORT_TABLE) {
+void with_table(const Table& tab, uint32_t count, Fill&& fill, Launch&& launch) {
+  if (count <= SHORT_TABLE) {
     Args<TensorTable<SHORT_TABLE>> a;
     fill(a);
-    shorten(tab, &a.tab);
+    shorten(tab, count, &a.tab);
     launch(a);
   } else {
     Args<TensorTable<TABLE>> a;
@@ -40,10 +40,10 @@ void with_table(const Table& tab, Fill&& fill, Launch&& launch) {
 template <int KIND>
 uint32_t run_partials(const thc_tensors* t, uint64_t bytes, bool in_place, double* partials, hipStream_t s) {
   uint32_t written = 0, keep = (uint32_t)(norm_keeps(bytes, in_place) >> LOG_NORM_UNIT);
-  for_tables(t, Grid::TENSOR, 0, 0, LOG_NORM_UNIT, [&](const TensorTable<TABLE>& tab, uint32_t units) {
+  for_tables(t, Grid::TENSOR, 0, 0, LOG_NORM_UNIT, [&](const TensorTable<TABLE>& tab, uint32_t count, uint32_t units) {
     const uint32_t groups = units < NORM_PARTIALS ? units : NORM_PARTIALS, kept = keep < units ? keep : units;
     with_table<NormArgs>(
-        tab,
+        tab, count,
         [&](auto& a) {
           a.partials = partials;
           a.units = units;
@@ -69,9 +69,9 @@ bool run_one(const thc_tensors* t, uint64_t bytes, bool in_place, NormOut o, hip
   if (bytes > ONE_MOST_UNITS << LOG_WAVE_UNIT || t->count > SHORT_TABLE) return false;
   OneArgs a;
   a.out = o;
-  a.units = a.tab.count = 0;
-  for_tables(t, Grid::TENSOR, 0, 0, LOG_WAVE_UNIT, [&](const TensorTable<TABLE>& tab, uint32_t units) {
-    shorten(tab, &a.tab);
+  a.units = 0;
+  for_tables(t, Grid::TENSOR, 0, 0, LOG_WAVE_UNIT, [&](const TensorTable<TABLE>& tab, uint32_t count, uint32_t units) {
+    shorten(tab, count, &a.tab);
     a.units = units;
   });
   if (a.units > ONE_MOST_UNITS) return false;
@@ -82,9 +82,9 @@ bool run_one(const thc_tensors* t, uint64_t bytes, bool in_place, NormOut o, hip
 
 template <class Launch>
 void run_moves(const thc_tensors* t, Grid grid, uint32_t flat_bytes, uint64_t zeros, void* flat, const float* scale, Launch&& launch) {
-  for_tables(t, grid, flat_bytes, zeros, LOG_MOVE_UNIT, [&](const TensorTable<TABLE>& tab, uint32_t units) {
+  for_tables(t, grid, flat_bytes, zeros, LOG_MOVE_UNIT, [&](const TensorTable<TABLE>& tab, uint32_t count, uint32_t units) {
     with_table<MoveArgs>(
-        tab,
+        tab, count,
         [&](auto& a) {
           a.flat = flat;
           a.scale = scale;
@@ -104,21 +104,21 @@ template <int KIND>
 void run_clip(const thc_tensors* t, NormOut o, double* partials, hipStream_t s) {
   const uint64_t bytes = list_bytes(t);
   if (run_one<KIND>(t, bytes, true, o, s)) return;
-  const uint32_t count = run_partials<KIND>(t, bytes, true, partials, s);
-  if (count <= FUSED_PARTIALS) {
-    for_tables(t, Grid::TENSOR, 0, 0, LOG_MOVE_UNIT, [&](const TensorTable<TABLE>& tab, uint32_t units) {
+  const uint32_t written = run_partials<KIND>(t, bytes, true, partials, s);
+  if (written <= FUSED_PARTIALS) {
+    for_tables(t, Grid::TENSOR, 0, 0, LOG_MOVE_UNIT, [&](const TensorTable<TABLE>& tab, uint32_t count, uint32_t units) {
       with_table<FinishArgs>(
-          tab,
+          tab, count,
           [&](auto& a) {
             a.out = o;
             a.partials = partials;
-            a.count = count;
+            a.count = written;
           },
           [&](const auto& a) { k_finish_scale<KIND><<<dim3(units), dim3(TNT), 0, s>>>(a); });
     });
     return;
   }
-  run_final<KIND>(FinalArgs{o, partials, count}, s);
+  run_final<KIND>(FinalArgs{o, partials, written}, s);
   run_moves(t, Grid::TENSOR, 0, 0, nullptr, o.scale, [&](const auto& a, dim3 grid) { k_scale<<<grid, dim3(TNT), 0, s>>>(a); });
 }
 

@@ -28,7 +28,7 @@ template <> __device__ __forceinline__ F16 narrow<F16>(float x) {
   return F16{(_Float16)x};
 }
 
-template <class T, int N>
+template <class T, uint32_t N>
 struct Pack { T x[N]; };
 
 template <int WORDS, int ALIGN> struct Words;
@@ -64,25 +64,23 @@ struct Piece {
   uint32_t type;
 };
 
-// Each wave counts the tensors that start at or before the unit, 64 at a time.
+// Each wave counts the tensors that start at or before the unit: a lane reads the starts of a few in one access.
 template <uint32_t LOG_UNIT, Grid GRID, uint32_t FLAT_BYTES, class Table>
 __device__ __forceinline__ Piece locate(const Table& tab, uint32_t u) {
-  const uint32_t lane = threadIdx.x & 63u;
+  const auto starts = reinterpret_cast<const Pack<uint32_t, Table::LANES>*>(tab.unit)[threadIdx.x & 63u];
   uint32_t n = 0;
 #pragma unroll
-  for (uint32_t k = 0; k < Table::SIZE; k += 64) {
-    const uint32_t unit = tab.unit[k + lane];    // all at once: no condition before the load
-    n += (uint32_t)__popcll(__ballot((k + lane < tab.count) & (unit <= u)));
-  }
+  for (uint32_t k = 0; k < Table::LANES; ++k) n += (uint32_t)__popcll(__ballot(starts.x[k] <= u));
   const uint32_t i = __builtin_amdgcn_readfirstlane(n - 1u);
+  const uint64_t w = tab.ptr[i], next = tab.ptr[i + 1];
+  const uint32_t lo = tab.at[i], lo_next = tab.at[i + 1];
   Piece p;
-  const uint64_t at = tab.at[i];
-  p.ptr = static_cast<char*>(tab.ptr[i]);
-  p.at = at & AT_MASK;
-  p.type = (uint32_t)(at >> AT_BITS);
+  p.ptr = (char*)(__attribute__((address_space(1))) char*)(w & PTR_MASK);   // global memory: a plain cast leaves that open, and the accesses slower
+  p.at = (w >> PTR_BITS & 0xFF) << 32 | lo;
+  p.type = (uint32_t)(w >> (PTR_BITS + 8));
   const uint32_t size = GRID == Grid::FLAT ? FLAT_BYTES : p.type == TYPE_F32 ? 4 : 2;
-  p.len = (int64_t)(((tab.at[i + 1] & AT_MASK) - p.at) * size);
-  const uint64_t addr = GRID == Grid::FLAT ? p.at * size : reinterpret_cast<uintptr_t>(p.ptr);
+  p.len = (int64_t)((((next >> PTR_BITS & 0xFF) << 32 | lo_next) - p.at) * size);
+  const uint64_t addr = GRID == Grid::FLAT ? p.at * size : w;
   p.lo = (int64_t)((uint64_t)(u - tab.unit[i]) << LOG_UNIT) - (int64_t)(addr % LINE);
   return p;
 }
@@ -191,11 +189,11 @@ __device__ __forceinline__ void norm_unit(const Piece& p, bool keep, A& acc) {
 
 template <class Table>
 struct NormArgs {
+  Table tab;
   double* partials;
   uint32_t units;
   uint32_t keep;        // units that the caches are to hold on to: the launch's first ones
   uint32_t before;      // partials that an earlier launch of the call has written: these are added to
-  Table tab;
 };
 static_assert(sizeof(NormArgs<TensorTable<TABLE>>) <= 4096, "kernel arguments");
 
@@ -306,9 +304,9 @@ __device__ __forceinline__ void scale_piece(const Piece& p, float c) {
 // flat: the vector, or null where the tensors are scaled in place
 template <class Table>
 struct MoveArgs {
+  Table tab;
   void* flat;
   const float* scale;   // or null
-  Table tab;
 };
 static_assert(sizeof(MoveArgs<TensorTable<TABLE>>) <= 4096, "kernel arguments");
 
@@ -317,10 +315,10 @@ constexpr uint32_t FUSED_PARTIALS = 384;
 
 template <class Table>
 struct FinishArgs {
+  Table tab;
   NormOut out;
   const double* partials;
   uint32_t count;
-  Table tab;
 };
 
 template <int KIND, class Table>
@@ -373,9 +371,9 @@ __global__ __launch_bounds__(TNT, 8) void k_scatter(const MoveArgs<Table> a) {
 constexpr uint32_t ONE_MOST_UNITS = 2 * ONE_NT / 64;
 
 struct OneArgs {
+  TensorTable<SHORT_TABLE> tab;
   NormOut out;
   uint32_t units;
-  TensorTable<SHORT_TABLE> tab;
 };
 
 template <int KIND, bool SCALE>

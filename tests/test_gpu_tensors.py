@@ -80,7 +80,8 @@ def _scaled(x, c):
 SIZES = {
     "none": [], "empty": [0, 0], "one": [1], "few": [0, 1, 2, 0, 3, 5, 8, 13], "unit": [8191, 8192, 8193],
     "odd": [7, 40001, 1, 129, 16385, 250, 3, 65537], "many": [1 + (i * 37) % 300 for i in range(700)],
-    "table": [33] * 192, "table_and_one": [33] * 193, "large": [3_000_001, 17, 1_500_000],
+    "table": [33] * 192, "table_and_one": [33] * 193, "63": [21] * 63, "64": [21] * 64, "244": [33] * 244, "245": [33] * 245, "489": [5] * 489,
+    "one_group": [32_768 - 32], "two_units_a_wave": [1000] * 32, "and_one": [1000] * 33, "fused": [3_000_000, 145_000], "large": [3_000_001, 17, 1_500_000],
 }
 LEADS = {"aligned": (0,), "odd": (1, 3, 0, 7, 2)}
 

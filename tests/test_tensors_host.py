@@ -1,5 +1,8 @@
 """Lists of tensors on the host: what the calls that take them refuse, before anything reaches a GPU."""
 import ctypes as C
+import os
+import shutil
+import subprocess
 import types
 
 import pytest
@@ -7,6 +10,7 @@ import torch
 
 from paper_2302_08545_amd import api
 
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 EINVAL, OK = -1, 0
 INF, NAN = float("inf"), float("nan")
 T430 = [0, 3, 5, 7, 9, 11, 13, 14, 15, 17, 19, 21, 23, 25, 27, 30]
@@ -39,6 +43,7 @@ def test_bad_lists_are_refused_by_every_call():
     _every(_raw([4096, 4098], [4, 4], [0, 0]))                # binary32 on two bytes
     _every(_raw([4097], [4], [1]))                            # bf16 on one byte
     _every(_raw([4096], [4], [3]))                            # no such type
+    _every(_raw([1 << 48], [4], [0]))                         # no device address
     _every(_raw([4096], [1 << 40], [0]))                      # too long, alone and together
     _every(_raw([4096, 1 << 43], [1 << 39, 1 << 39], [1, 1]))
     n = C.c_uint64(4)
@@ -169,3 +174,19 @@ def test_buffers_of_another_type_size_or_place_are_refused():
             api.thc_scatter(p, flat, None, t, stream=0)
     with pytest.raises(ValueError, match="grad_out"):
         api.thc_gather(_p(in_dtype=1), t, None, _gpu(torch.zeros(1 << 12)), stream=0)
+
+
+def test_tables_of_a_list_are_clean_under_asan_and_ubsan(tmp_path):
+    """The tables that travel with the launches, walked on the CPU as the kernels walk them: every element once, nothing outside."""
+    gxx = shutil.which("g++")
+    if gxx is None:
+        pytest.skip("no g++")
+    exe = tmp_path / "san_tensors"
+    subprocess.run([gxx, "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=all", "-static-libasan",
+                    "-static-libubsan", "-Wall", "-Wextra", "-Werror", "-I", os.path.join(ROOT, "include"), "-I",
+                    os.path.join(ROOT, "paper_2302_08545_amd", "csrc"), os.path.join(ROOT, "tests", "san_tensors.cpp"), "-o", str(exe)],
+                   check=True, capture_output=True, text=True)
+    env = dict(os.environ, ASAN_OPTIONS="detect_leaks=1:abort_on_error=0", UBSAN_OPTIONS="print_stacktrace=1")
+    res = subprocess.run([str(exe)], capture_output=True, text=True, env=env, timeout=300)
+    assert res.returncode == 0, res.stdout + res.stderr
+    assert "0 problem(s)" in res.stdout
