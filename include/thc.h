@@ -215,7 +215,9 @@ int thc_uniform_decompress(const thc_params* p, uint64_t round, const void* agg,
  * travels by value with the launches, so the arrays of thc_tensors are read during the call only).
  *
  * A list may hold up to 2^40 - 1 elements.  Every tensor is one run of memory, aligned to its own element type,
- * and is taken in the order of its memory.  Tensors without elements are allowed (their pointer may be null). */
+ * and is taken in the order of its memory.  Tensors without elements are allowed (their pointer may be null).
+ * norm_out, scale_out and ws must overlap neither each other nor the tensors, and `scale` nothing that is written
+ * (THC_EINVAL). */
 typedef struct thc_tensors {
   uint64_t count;
   void* const* data;     /* host array of device pointers */

@@ -917,7 +917,7 @@ const char* const kNames[] = {"THC_OK", "THC_EINVAL", "THC_ETABLE", "THC_EOVERFL
 
 extern "C" {
 
-int thc_version(void) { return 200; }
+int thc_version(void) { return 300; }
 
 const char* thc_strerror(int status) {
   const int i = -status;

@@ -4,7 +4,8 @@
 
 #include <algorithm>
 #include <cstdint>
-#include <new>
+#include <initializer_list>
+#include <utility>
 #include <vector>
 
 #include "thc.h"
@@ -14,6 +15,10 @@ namespace thc {
 // The work of a launch is counted in units of a power of two of bytes.  A tensor's units lie on a grid that starts on a 128-byte
 // line of what the kernel accesses in whole lines (its own memory, or its place in the flat vector), up to one line before its first
 // element, so that no line but a tensor's first and last is shared by two units.
+// A move has a workgroup for each unit, in the order of memory, so that consecutive workgroups, which go to the eight XCDs in turn, write
+// consecutive 8 KB: us by the unit's bytes, 4 / 8 / 16 / 32 KB, scatter of 553 MB in binary32 176.9 / 180 / 182 / 188, gather of 3.1 GB in
+// bf16 1077 / 1040 / 1047 / 1081 (2048 workgroups that walk the units: 202 and 1199).  The norm is indifferent from 16 KB on (3.1 GB 464 us
+// at 16 KB, 461 at 32; 546 at 8 KB) and takes long units, since its workgroups keep sums.
 constexpr uint32_t LINE = 128;
 constexpr uint32_t LOG_NORM_UNIT = 15, LOG_MOVE_UNIT = 13, LOG_WAVE_UNIT = 12;
 
@@ -33,7 +38,7 @@ enum { TYPE_F32 = THC_DTYPE_F32, TYPE_BF16 = THC_DTYPE_BF16, TYPE_F16 = THC_DTYP
 
 template <uint32_t N>
 struct TensorTable {
-  static constexpr uint32_t SIZE = N, LANES = (N + 64) / 64;   // places that one of 64 lanes looks at
+  static constexpr uint32_t LANES = (N + 64) / 64;   // places that one of 64 lanes looks at
   uint32_t unit[64 * LANES];   // each tensor's first unit; behind the last one no unit is as large
   uint64_t ptr[N + 1];         // address; above PTR_BITS the upper 8 bits of the place in the flat vector, then the type
   uint32_t at[N + 1];          // the lower 32 bits of the first element's place in the flat vector; behind the last tensor its end
@@ -89,18 +94,24 @@ inline uint64_t norm_keeps(uint64_t bytes, bool in_place) {
   return (bytes >= 768ull << 20 ? 384ull : 256ull) << 20;
 }
 
-// Whether memory that a call writes overlaps other memory of the call: the tensors each other (`each_other`), or the range
-// [flat, flat + bytes).  THC_EINVAL if so.
-inline int check_overlap(const thc_tensors* t, bool each_other, const void* flat, uint64_t bytes) {
-  const uintptr_t f0 = reinterpret_cast<uintptr_t>(flat), f1 = f0 + bytes;
+struct Range {
+  uintptr_t begin, end;
+  Range(const void* p, uint64_t bytes) : begin(reinterpret_cast<uintptr_t>(p)), end(begin + (p ? bytes : 0)) {}
+  bool meets(const Range& r) const { return begin < r.end && r.begin < end; }
+};
+
+// Whether memory that a call writes overlaps other memory of the call: the tensors each other (`each_other`), or `others`, among which the
+// caller has seen to it that nothing overlaps.  THC_EINVAL if so.
+inline int check_overlap(const thc_tensors* t, bool each_other, std::initializer_list<Range> others) {
   bool sorted = true;
   uintptr_t last = 0;
   for (uint64_t i = 0; i < t->count; ++i) {
     if (!t->numel[i]) continue;
-    const uintptr_t a = reinterpret_cast<uintptr_t>(t->data[i]), b = a + t->numel[i] * type_bytes(t->dtype[i]);
-    if (a < f1 && f0 < b) return THC_EINVAL;
-    sorted = sorted && a >= last;
-    last = b;
+    const Range r(t->data[i], t->numel[i] * type_bytes(t->dtype[i]));
+    for (const Range& o : others)
+      if (r.meets(o)) return THC_EINVAL;
+    sorted = sorted && r.begin >= last;
+    last = r.end;
   }
   if (!each_other || sorted) return THC_OK;      // in the order of their addresses, one behind the other: nothing left to compare
   try {
@@ -113,7 +124,7 @@ inline int check_overlap(const thc_tensors* t, bool each_other, const void* flat
     std::sort(r.begin(), r.end());
     for (size_t i = 1; i < r.size(); ++i)
       if (r[i].first < r[i - 1].second) return THC_EINVAL;
-  } catch (const std::bad_alloc&) {
+  } catch (...) {                                // no memory for it: nothing is thrown through the C entry
     return THC_EUNSUPPORTED;
   }
   return THC_OK;

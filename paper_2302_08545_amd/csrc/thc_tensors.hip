@@ -10,14 +10,19 @@ using namespace thc;
 
 bool aligned(const void* p, uintptr_t to) { return p && reinterpret_cast<uintptr_t>(p) % to == 0; }
 
-int check_norm(const thc_tensors* t, int kind, float max_norm, const float* norm_out, const float* scale_out, const void* ws) {
+constexpr size_t NORM_WS_BYTES = NORM_PARTIALS * sizeof(double) + 16;   // partials, and the factor where the caller keeps none
+
+int check_norm(const thc_tensors* t, int kind, float max_norm, const float* norm_out, const float* scale_out, const void* ws,
+               bool in_place) {
   uint64_t total = 0;
   const int rc = validate_tensors(t, &total);
   if (rc) return rc;
   if (kind != THC_NORM_L2 && kind != THC_NORM_MAX) return THC_EINVAL;
   if (!(max_norm >= 0.f) || !aligned(norm_out, 4) || !aligned(ws, 16)) return THC_EINVAL;
   if (scale_out && !aligned(scale_out, 4)) return THC_EINVAL;
-  return THC_OK;
+  const Range norm(norm_out, sizeof(float)), scale(scale_out, sizeof(float)), work(ws, NORM_WS_BYTES);
+  if (norm.meets(scale) || norm.meets(work) || scale.meets(work)) return THC_EINVAL;
+  return check_overlap(t, in_place, {norm, scale, work});
 }
 
 // launch(arguments) with the table in the smaller form that holds it
@@ -129,7 +134,9 @@ int check_flat(const thc_params* p, const thc_tensors* t, const void* flat, uint
   rc = validate_tensors(t, total);
   if (rc) return rc;
   if (*total > p->d || !aligned(flat, 16) || (scale && !aligned(scale, 4))) return THC_EINVAL;
-  return check_overlap(t, to_tensors, flat, p->d * flat_bytes);
+  const Range vector(flat, p->d * flat_bytes), factor(scale, sizeof(float));
+  if (!to_tensors) return factor.meets(vector) ? (int)THC_EINVAL : check_overlap(t, false, {vector});
+  return check_overlap(t, true, {vector, factor});
 }
 
 }  // namespace
@@ -138,12 +145,12 @@ extern "C" {
 
 int thc_norm_workspace_bytes(size_t* bytes_out) {
   if (!bytes_out) return THC_EINVAL;
-  *bytes_out = NORM_PARTIALS * sizeof(double) + 16;   // partials, and the factor where the caller keeps none
+  *bytes_out = NORM_WS_BYTES;
   return THC_OK;
 }
 
 int thc_grad_norm(const thc_tensors* t, int kind, float max_norm, float* norm_out, float* scale_out, void* ws, void* stream) {
-  const int rc = check_norm(t, kind, max_norm, norm_out, scale_out, ws);
+  const int rc = check_norm(t, kind, max_norm, norm_out, scale_out, ws, false);
   if (rc) return rc;
   const NormOut o{norm_out, scale_out, max_norm};
   double* const partials = static_cast<double*>(ws);
@@ -154,9 +161,7 @@ int thc_grad_norm(const thc_tensors* t, int kind, float max_norm, float* norm_ou
 }
 
 int thc_grad_clip(const thc_tensors* t, int kind, float max_norm, float* norm_out, float* scale_out, void* ws, void* stream) {
-  int rc = check_norm(t, kind, max_norm, norm_out, scale_out, ws);
-  if (rc) return rc;
-  rc = check_overlap(t, true, nullptr, 0);
+  const int rc = check_norm(t, kind, max_norm, norm_out, scale_out, ws, true);
   if (rc) return rc;
   hipStream_t s = static_cast<hipStream_t>(stream);
   double* const partials = static_cast<double*>(ws);

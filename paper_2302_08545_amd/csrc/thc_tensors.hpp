@@ -1,6 +1,11 @@
 // Kernels between a model's tensors and the flat vectors of the path: the global norm of a list of tensors, scaling it in place,
-// gathering it into a flat vector and scattering one over it.  All are bound by memory; none has more than one operation per
-// element but for the norm's conversion and multiply-add in binary64.
+// gathering it into a flat vector and scattering one over it.
+//
+//   norm     v = sqrt(sum x^2) in binary64, or max |x|;  c = 1 where v <= max_norm, else max_norm / v, rounded once to binary32
+//   moves    y = round(fl32(x * c)): the product rounded to binary32, then to the type, as elementary operations would
+//
+// Bound by memory, with one operation per element (the norm: a conversion and a multiply-add in binary64, a quarter of the ALU at full
+// rate); small lists by launches.  Rates of large lists (MI355X; a copy reaches 6.0 TB/s): the norm reads 6.8 TB/s, moves 6.0 to 6.4.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -12,7 +17,9 @@
 namespace thc {
 
 constexpr int TNT = 256;                   // threads per workgroup
-constexpr uint32_t NORM_PARTIALS = 8192;   // most workgroups of a norm launch: one partial each
+// Most workgroups of a norm launch, one partial each: 3.1 GB in bf16 467 us with 2048, 461 with 8192, 460 with 16384 (672 MB 110.4 / 109.1 /
+// 110.7).
+constexpr uint32_t NORM_PARTIALS = 8192;
 constexpr int FINAL_NT = 1024, ONE_NT = 1024;
 
 struct Bf16 { uint16_t bits; };
@@ -197,6 +204,7 @@ struct NormArgs {
 };
 static_assert(sizeof(NormArgs<TensorTable<TABLE>>) <= 4096, "kernel arguments");
 
+// Seven workgroups to a compute unit: with registers for eight the magnitudes' form spills (672 MB of f16 125 us instead of 109).
 template <int KIND, class Table>
 __global__ __launch_bounds__(TNT, 7) void k_norm(const NormArgs<Table> a) {
   Acc<KIND> acc;
@@ -310,7 +318,8 @@ struct MoveArgs {
 };
 static_assert(sizeof(MoveArgs<TensorTable<TABLE>>) <= 4096, "kernel arguments");
 
-// The same from up to FUSED_PARTIALS partials, which each wave adds up by itself: the launch of k_norm_final is saved.
+// The scaling behind up to FUSED_PARTIALS partials, which each wave adds up by itself: the launch of k_norm_final is saved.  Clipping of one
+// binary32 tensor, us without / with: 256 KB 5.9 / 4.5, 2 MB 6.6 / 5.3, 8 MB (257 partials) 7.1 / 6.2, 16 MB (513) 8.5 / 8.6.
 constexpr uint32_t FUSED_PARTIALS = 384;
 
 template <class Table>

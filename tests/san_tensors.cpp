@@ -138,19 +138,24 @@ int main() {
     check_cover(l, Grid::TENSOR, 0, 0, LOG_MOVE_UNIT, 8);
     for (uint32_t b : {2u, 4u}) check_cover(l, Grid::FLAT, b, zeros, LOG_MOVE_UNIT, round % 2 ? 16 : 8);
     const thc_tensors t = l.get();
-    check(check_overlap(&t, true, nullptr, 0) == THC_OK, "overlap where there is none");
+    check(check_overlap(&t, true, {}) == THC_OK, "overlap where there is none");
     if (count > 1) {                           // in another order, and then one of them twice
       std::swap(l.data.front(), l.data.back());
       std::swap(l.numel.front(), l.numel.back());
       std::swap(l.dtype.front(), l.dtype.back());
       const thc_tensors s = l.get();
-      check(check_overlap(&s, true, nullptr, 0) == THC_OK, "overlap where there is none, in another order");
+      check(check_overlap(&s, true, {}) == THC_OK, "overlap where there is none, in another order");
       for (int i = 0; i < count; ++i)
         if (l.numel[i]) {
+          const char* const p = static_cast<char*>(l.data[i]);
+          const uint64_t n = l.numel[i] * type_bytes(l.dtype[i]);
+          check(check_overlap(&s, false, {Range(nullptr, 4), Range(p + n - 1, 1)}) == THC_EINVAL, "range over a tensor's end not seen");
+          check(check_overlap(&s, false, {Range(p - 3, 4)}) == THC_EINVAL, "range over a tensor's start not seen");
+          check(check_overlap(&s, false, {Range(reinterpret_cast<void*>(1 << 19), 1 << 19)}) == THC_OK, "range in front of the list");
           l.add(reinterpret_cast<uintptr_t>(l.data[i]) + (l.numel[i] - 1) * type_bytes(l.dtype[i]), 1, l.dtype[i]);
           const thc_tensors d = l.get();
-          check(check_overlap(&d, true, nullptr, 0) == THC_EINVAL, "overlap not seen");
-          check(check_overlap(&d, false, nullptr, 0) == THC_OK, "overlap of what is only read");
+          check(check_overlap(&d, true, {}) == THC_EINVAL, "overlap not seen");
+          check(check_overlap(&d, false, {}) == THC_OK, "overlap of what is only read");
           break;
         }
     }

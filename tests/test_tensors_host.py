@@ -12,6 +12,7 @@ from paper_2302_08545_amd import api
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 EINVAL, OK = -1, 0
+NORM, SCALE, WS = 1 << 45, (1 << 45) + 4, 1 << 46      # addresses that no list here comes near
 INF, NAN = float("inf"), float("nan")
 T430 = [0, 3, 5, 7, 9, 11, 13, 14, 15, 17, 19, 21, 23, 25, 27, 30]
 
@@ -31,8 +32,8 @@ def _every(t, p=None, want=EINVAL):
     """All four calls with this list and otherwise good arguments."""
     L, p = api.lib(), p or _p()
     r = C.byref(t) if t is not None else None
-    assert L.thc_grad_norm(r, 0, 1.0, 16, 16, 16, None) == want
-    assert L.thc_grad_clip(r, 0, 1.0, 16, 16, 16, None) == want
+    assert L.thc_grad_norm(r, 0, 1.0, NORM, SCALE, WS, None) == want
+    assert L.thc_grad_clip(r, 0, 1.0, NORM, SCALE, WS, None) == want
     assert L.thc_gather(C.byref(p), r, None, 1 << 44, None) == want
     assert L.thc_scatter(C.byref(p), 1 << 44, None, r, None) == want
 
@@ -55,17 +56,25 @@ def test_bad_lists_are_refused_by_every_call():
 @pytest.mark.parametrize("call", ["thc_grad_norm", "thc_grad_clip"])
 def test_arguments_of_the_norm_calls(call):
     f, t = getattr(api.lib(), call), C.byref(_raw([4096], [4], [0]))
-    assert f(t, 2, 1.0, 16, 16, 16, None) == EINVAL and f(t, -1, 1.0, 16, 16, 16, None) == EINVAL
-    assert f(t, 0, -1.0, 16, 16, 16, None) == EINVAL and f(t, 0, NAN, 16, 16, 16, None) == EINVAL
-    assert f(t, 0, 1.0, None, 16, 16, None) == EINVAL and f(t, 0, 1.0, 18, 16, 16, None) == EINVAL
-    assert f(t, 0, 1.0, 16, 18, 16, None) == EINVAL
-    assert f(t, 0, 1.0, 16, 16, None, None) == EINVAL and f(t, 0, 1.0, 16, 16, 24, None) == EINVAL
+    assert f(t, 2, 1.0, NORM, SCALE, WS, None) == EINVAL and f(t, -1, 1.0, NORM, SCALE, WS, None) == EINVAL
+    assert f(t, 0, -1.0, NORM, SCALE, WS, None) == EINVAL and f(t, 0, NAN, NORM, SCALE, WS, None) == EINVAL
+    assert f(t, 0, 1.0, None, SCALE, WS, None) == EINVAL and f(t, 0, 1.0, NORM + 2, SCALE + 4, WS, None) == EINVAL
+    assert f(t, 0, 1.0, NORM, SCALE + 2, WS, None) == EINVAL
+    assert f(t, 0, 1.0, NORM, SCALE, None, None) == EINVAL and f(t, 0, 1.0, NORM, SCALE, WS + 8, None) == EINVAL
+    # what is written lies apart: from each other, and from the tensors
+    assert f(t, 0, 1.0, NORM, NORM, WS, None) == EINVAL
+    end = WS + api.thc_norm_workspace_bytes() - 4
+    assert f(t, 0, 1.0, end, SCALE, WS, None) == EINVAL and f(t, 0, 1.0, NORM, end, WS, None) == EINVAL
+    assert f(t, 0, 1.0, 4096, SCALE, WS, None) == EINVAL and f(t, 0, 1.0, NORM, 4096 + 12, WS, None) == EINVAL
+    assert f(t, 0, 1.0, NORM, None, 4096, None) == EINVAL
 
 
 def test_arguments_of_the_flat_calls():
     L, p, t = api.lib(), C.byref(_p()), C.byref(_raw([4096], [4], [0]))
     assert L.thc_gather(p, t, None, None, None) == EINVAL and L.thc_gather(p, t, None, (1 << 44) + 8, None) == EINVAL
     assert L.thc_gather(p, t, 18, 1 << 44, None) == EINVAL
+    assert L.thc_gather(p, t, (1 << 44) + 8, 1 << 44, None) == EINVAL          # a factor inside what is written
+    assert L.thc_scatter(p, 1 << 44, 4096 + 12, t, None) == EINVAL
     assert L.thc_scatter(p, None, None, t, None) == EINVAL and L.thc_scatter(p, (1 << 44) + 8, None, t, None) == EINVAL
     assert L.thc_scatter(p, 1 << 44, 18, t, None) == EINVAL
     # one element more than the vector holds
@@ -87,7 +96,7 @@ def test_arguments_of_the_flat_calls():
 ])
 def test_memory_written_twice_is_refused(data, numel, dtype):
     L, t = api.lib(), _raw(data, numel, dtype)
-    assert L.thc_grad_clip(C.byref(t), 0, 1.0, 16, 16, 16, None) == EINVAL
+    assert L.thc_grad_clip(C.byref(t), 0, 1.0, NORM, SCALE, WS, None) == EINVAL
     assert L.thc_scatter(C.byref(_p(d=1 << 20)), 1 << 44, None, C.byref(t), None) == EINVAL
 
 
@@ -147,7 +156,7 @@ def test_lists_of_another_device_than_the_current_one_are_refused(monkeypatch):
     t = api.make_tensors([_gpu(torch.zeros(4), at=1)])
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
     monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
-    for call in (lambda: api.thc_grad_norm(t, 0, 1.0, 16, 16, 16), lambda: api.thc_grad_clip(t, 0, 1.0, 16, 16, 16),
+    for call in (lambda: api.thc_grad_norm(t, 0, 1.0, NORM, SCALE, WS), lambda: api.thc_grad_clip(t, 0, 1.0, NORM, SCALE, WS),
                  lambda: api.thc_gather(_p(), t, None, 1 << 44), lambda: api.thc_scatter(_p(), 1 << 44, None, t)):
         with pytest.raises(ValueError, match="cuda:1"):
             call()
