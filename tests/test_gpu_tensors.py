@@ -333,3 +333,65 @@ def test_a_training_step_of_four_workers(dtype):
         assert torch.equal(g.cpu(), out[pos:pos + y.numel()].cpu().to(y.dtype))
         pos += y.numel()
     Y.guards_hold()
+
+
+@pytest.mark.parametrize("sizes", [[5000], [300_000, 17], [9_000_000, 33, 4_000_000], [600] * 300], ids=["one_group", "fused", "launches", "tables"])
+def test_clipping_without_a_place_for_the_factor(sizes):
+    cpu = _values(sizes, (F32, BF16), seed=31)
+    X, Y = Tensors(cpu, (1, 0)), Tensors(cpu, (1, 0))
+    v = _norm64(cpu, api.THC_NORM_L2)
+    norm, scale, ws = _scalars()
+    api.thc_grad_clip(X.gpu, api.THC_NORM_L2, v / 3, norm, scale, ws)
+    n2, _, w2 = _scalars()
+    api.thc_grad_clip(Y.gpu, api.THC_NORM_L2, v / 3, n2, None, w2)
+    assert torch.equal(norm, n2) and abs(float(norm) - v) <= v * NORM_REL
+    for x, a, b in zip(cpu, X.gpu, Y.gpu):
+        assert torch.equal(a, b) and torch.equal(a.cpu(), _scaled(x, float(scale)))
+    X.guards_hold()
+    Y.guards_hold()
+
+
+def test_a_tensor_listed_twice_is_read_twice():
+    x = torch.randn(10_000, generator=torch.Generator().manual_seed(8))
+    g = x.to(DEV)
+    t = api.make_tensors([g, g[:100], g])
+    norm, scale, ws = _scalars()
+    api.thc_grad_norm(t, api.THC_NORM_L2, INF, norm, scale, ws)
+    v = _norm64([x, x[:100], x], api.THC_NORM_L2)
+    assert abs(float(norm) - v) <= v * NORM_REL
+    p = api.make_params(20 * 1024, 1024, 1, 4, 15, 2.0, 7, range(16))
+    flat = torch.empty(20 * 1024, device=DEV)
+    api.thc_gather(p, t, None, flat)
+    assert torch.equal(flat[:20_100].cpu(), torch.cat([x, x[:100], x]))
+    for call in (lambda: api.thc_grad_clip(t, api.THC_NORM_L2, 1.0, norm, scale, ws), lambda: api.thc_scatter(p, flat, None, t)):
+        with pytest.raises(api.ThcError) as e:
+            call()
+        assert e.value.status == -1
+    torch.cuda.synchronize()
+    assert torch.equal(g.cpu(), x)
+
+
+def test_estimates_beyond_f16_and_in_its_subnormal_range():
+    est = torch.tensor([1e5, -7e4, 65504.0, 65519.0, 65520.0, 3e-8, 2.0 ** -25, 3 * 2.0 ** -25, -1e-30, 0.1, NAN, INF] + [0.0] * 1012)
+    y = torch.full((12,), 5.0, dtype=F16, device=DEV)
+    z = torch.full((12,), 5.0, dtype=BF16, device=DEV)
+    p = api.make_params(1024, 1024, 1, 4, 15, 2.0, 7, range(16))
+    api.thc_scatter(p, est.to(DEV), None, [y])
+    api.thc_scatter(p, est.to(DEV), None, [z])
+    assert np.array_equal(y.float().cpu().numpy(), est[:12].to(F16).float().numpy(), equal_nan=True)
+    assert np.array_equal(z.float().cpu().numpy(), est[:12].to(BF16).float().numpy(), equal_nan=True)
+
+
+def test_on_a_stream_of_the_callers_own():
+    side = torch.cuda.Stream()
+    cpu = _values([70_000, 5], (BF16, F32), seed=41)
+    X = Tensors(cpu)
+    norm, scale, ws = _scalars()
+    p = api.make_params(69 * 1024, 1024, 1, 4, 15, 2.0, 7, range(16))
+    flat = torch.zeros(69 * 1024, device=DEV)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):                    # the current stream, and the same one by name
+        api.thc_grad_norm(X.gpu, api.THC_NORM_L2, 1.0, norm, scale, ws)
+    api.thc_gather(p, X.gpu, scale, flat, stream=side)
+    side.synchronize()
+    assert torch.equal(flat[:70_005].cpu(), torch.cat([x.float() * scale.cpu() for x in cpu]))
