@@ -22,6 +22,12 @@ struct List {
   thc_tensors get() const { return {data.size(), data.data(), numel.data(), dtype.data()}; }
 };
 
+static int overlap(const thc_tensors* t, bool each_other, std::initializer_list<Range> others) {
+  Scan scan;
+  const int rc = scan_tensors(t, &scan);
+  return rc ? rc : check_overlap(t, scan, each_other, others);
+}
+
 static int problems = 0;
 static void check(bool ok, const char* what, long long a = 0, long long b = 0) {
   if (ok) return;
@@ -44,15 +50,18 @@ static void walk_unit(int64_t lo, int64_t len, uint32_t log_unit, int slot, int 
 // Every element of a short list is taken once, in the units that locate() would find for it, and lies where the list has it.
 static void check_cover(const List& l, Grid grid, uint32_t flat_bytes, uint64_t zeros, uint32_t log_unit, int slot16) {
   const thc_tensors t = l.get();
-  uint64_t total = 0;
-  check(validate_tensors(&t, &total) == THC_OK, "refused");
+  Scan scan;
+  check(scan_tensors(&t, &scan) == THC_OK, "refused");
+  const uint64_t total = scan.total;
   std::vector<int> seen(total + zeros, 0);
   std::vector<uint64_t> address(total + zeros, 0);
   for (uint64_t i = 0, pos = 0; i < t.count; ++i)
     for (uint64_t j = 0; j < t.numel[i]; ++j) address[pos++] = reinterpret_cast<uintptr_t>(t.data[i]) + j * type_bytes(t.dtype[i]);
   uint32_t most = 0, least = ~0u, launches = 0;
-  for_tables(&t, grid, flat_bytes, zeros, log_unit, [&](const TensorTable<TABLE>& tab, uint32_t count, uint32_t units) {
+  uint64_t entries = 0, bytes = 0;
+  for_tables(&t, scan, grid, flat_bytes, zeros, log_unit, [&](const TensorTable<TABLE>& tab, uint32_t count, uint32_t units) {
     ++launches;
+    entries += count;
     most = count > most ? count : most;
     least = count < least ? count : least;
     check(count >= 1 && count <= TABLE, "tensors of a table", count);
@@ -88,6 +97,8 @@ static void check_cover(const List& l, Grid grid, uint32_t flat_bytes, uint64_t 
       });
     }
   });
+  for (uint64_t i = 0; i < t.count; ++i) bytes += t.numel[i] * type_bytes(t.dtype[i]);
+  check(entries == scan.entries + (zeros != 0) && bytes == scan.bytes, "entries or bytes", (long long)entries, (long long)scan.entries);
   for (uint64_t e = 0; e < seen.size(); ++e) check(seen[e] == 1, "element not taken once", (long long)e, seen[e]);
   check(launches < 2 || most - least <= launches, "launches of different lengths", most, least);
 }
@@ -99,12 +110,14 @@ static void check_long() {
   l.add((1ull << 33) + 4, (3ull << 33) + 7, THC_DTYPE_F32);
   l.add(1ull << 40, 3ull << 34, THC_DTYPE_BF16);
   const thc_tensors t = l.get();
-  uint64_t total = 0, sum = 0, next = 0;
-  check(validate_tensors(&t, &total) == THC_OK, "long list refused");
+  uint64_t sum = 0, next = 0;
+  Scan scan;
+  check(scan_tensors(&t, &scan) == THC_OK, "long list refused");
+  const uint64_t total = scan.total;
   int launches = 0;
   for (Grid grid : {Grid::TENSOR, Grid::FLAT}) {
     sum = next = 0;
-    for_tables(&t, grid, 4, 9, LOG_MOVE_UNIT, [&](const TensorTable<TABLE>& tab, uint32_t count, uint32_t units) {
+    for_tables(&t, scan, grid, 4, 9, LOG_MOVE_UNIT, [&](const TensorTable<TABLE>& tab, uint32_t count, uint32_t units) {
       ++launches;
       check(units && units <= MOST_UNITS && (uint64_t)units * 256 < 1ull << 32, "units of a launch", units);
       auto place = [&](uint32_t k) { return (tab.ptr[k] >> PTR_BITS & 0xFF) << 32 | tab.at[k]; };
@@ -138,24 +151,24 @@ int main() {
     check_cover(l, Grid::TENSOR, 0, 0, LOG_MOVE_UNIT, 8);
     for (uint32_t b : {2u, 4u}) check_cover(l, Grid::FLAT, b, zeros, LOG_MOVE_UNIT, round % 2 ? 16 : 8);
     const thc_tensors t = l.get();
-    check(check_overlap(&t, true, {}) == THC_OK, "overlap where there is none");
+    check(overlap(&t, true, {}) == THC_OK, "overlap where there is none");
     if (count > 1) {                           // in another order, and then one of them twice
       std::swap(l.data.front(), l.data.back());
       std::swap(l.numel.front(), l.numel.back());
       std::swap(l.dtype.front(), l.dtype.back());
       const thc_tensors s = l.get();
-      check(check_overlap(&s, true, {}) == THC_OK, "overlap where there is none, in another order");
+      check(overlap(&s, true, {}) == THC_OK, "overlap where there is none, in another order");
       for (int i = 0; i < count; ++i)
         if (l.numel[i]) {
           const char* const p = static_cast<char*>(l.data[i]);
           const uint64_t n = l.numel[i] * type_bytes(l.dtype[i]);
-          check(check_overlap(&s, false, {Range(nullptr, 4), Range(p + n - 1, 1)}) == THC_EINVAL, "range over a tensor's end not seen");
-          check(check_overlap(&s, false, {Range(p - 3, 4)}) == THC_EINVAL, "range over a tensor's start not seen");
-          check(check_overlap(&s, false, {Range(reinterpret_cast<void*>(1 << 19), 1 << 19)}) == THC_OK, "range in front of the list");
+          check(overlap(&s, false, {Range(nullptr, 4), Range(p + n - 1, 1)}) == THC_EINVAL, "range over a tensor's end not seen");
+          check(overlap(&s, false, {Range(p - 3, 4)}) == THC_EINVAL, "range over a tensor's start not seen");
+          check(overlap(&s, false, {Range(reinterpret_cast<void*>(1 << 19), 1 << 19)}) == THC_OK, "range in front of the list");
           l.add(reinterpret_cast<uintptr_t>(l.data[i]) + (l.numel[i] - 1) * type_bytes(l.dtype[i]), 1, l.dtype[i]);
           const thc_tensors d = l.get();
-          check(check_overlap(&d, true, {}) == THC_EINVAL, "overlap not seen");
-          check(check_overlap(&d, false, {}) == THC_OK, "overlap of what is only read");
+          check(overlap(&d, true, {}) == THC_EINVAL, "overlap not seen");
+          check(overlap(&d, false, {}) == THC_OK, "overlap of what is only read");
           break;
         }
     }
