@@ -17,8 +17,11 @@ namespace thc {
 // element, so that no line but a tensor's first and last is shared by two units.
 // A move has a workgroup for each unit, in the order of memory, so that consecutive workgroups, which go to the eight XCDs in turn, write
 // consecutive 8 KB: us by the unit's bytes, 4 / 8 / 16 / 32 KB, scatter of 553 MB in binary32 176.9 / 180 / 182 / 188, gather of 3.1 GB in
-// bf16 1077 / 1040 / 1047 / 1081 (2048 workgroups that walk the units: 202 and 1199).  The norm is indifferent from 16 KB on (3.1 GB 464 us
-// at 16 KB, 461 at 32; 546 at 8 KB) and takes long units, since its workgroups keep sums.
+// bf16 1077 / 1040 / 1047 / 1081 (256 to 2048 workgroups that walk the units: 183 to 219, and 1130 to 1254).
+// The norm has one workgroup of 512 threads on each of the 256 compute units, which walk the units together: 8 MB in flight are enough, and
+// memory answers fewer at a time faster.  us, 1.5 GB in binary32 / bf16: 256 x 512 threads with units of 16 KB 336 / 367, 32 KB 229 / 229,
+// 64 KB 240 / 241; 256 x 256 threads 227 / 249 (the multiply-adds of bf16 then take longer than its bytes); 256 x 1024 240 / 243;
+// 512 x 256 241 / 241; 1792 x 256 239 / 242; 8192 x 256 237 / 238.  256 MB, plainly read: 256 x 512 44.8 / 45.2, 8192 x 256 48.1 / 48.7.
 constexpr uint32_t LINE = 128;
 constexpr uint32_t LOG_NORM_UNIT = 15, LOG_MOVE_UNIT = 13, LOG_WAVE_UNIT = 12;
 
@@ -96,17 +99,21 @@ inline int scan_tensors(const thc_tensors* t, Scan* out) {
 }
 
 // Bytes at the start of a list that the norm's pass reads with plain loads, so that the 256 MB memory-side cache holds them for the
-// call that moves the list next; the rest is read non-temporally, which is 10 % faster and does not push out what is kept.
+// call that moves the list next; the rest is read non-temporally, which is 7 % faster and does not push out what is kept.
 // us on one binary32 tensor, nothing kept / 256 MB kept / all kept:
-//              48 MB                  96 MB                  224 MB                  320 MB                  512 MB                 1 GB
-//   norm      13.0 / 13.5            20.2 / 21.9            40.5 / 44.5             55.0 / 59.1 / 60.9      84.6 / 86.2 / 94.6     162 / 163 / 182
-//   + gather  31.4 / 29.0            53.9 / 50.6           115.5 / 109.4           161.6 / 152.8 / 154.7   256.4 / 244.0 / 254.3   508 / 497 / 511
-//   clip      32.7 / 33.0 (16 MB 17.7 / 20.2)  54.5 / 53.4  116.6 / 111.4          164.0 / 154.3 / 156.7   259.6 / 247.2 / 253.0   511 / 501 / 509
-// 384 MB kept: 1 GB 493 (gather) and 494, 512 MB 244.4 and 244.3 but the norm itself 90.1, 320 MB 154.9 and 156.7.
-inline uint64_t norm_keeps(uint64_t bytes, bool in_place) {
-  if (in_place && bytes < 64ull << 20) return 0;
-  return (bytes >= 768ull << 20 ? 384ull : 256ull) << 20;
-}
+//              16 MB         32 MB          64 MB          96 MB         224 MB          320 MB                  512 MB                  1 GB
+//   norm      8.1 / 8.1    10.0 / 10.5    14.3 / 15.5    18.9 / 20.4    37.1 / 39.9     51.0 / 53.9 / 54.7      78.6 / 81.8 / 86.0      152 / 155 / 169
+//   + gather 16.7 / 14.5   23.8 / 21.0    38.4 / 35.1    53.3 / 48.9   113.3 / 104.8   159.1 / 147.6 / 149.9   253.3 / 241.4 / 245.5   507 / 496 / 509
+//   clip     14.7 / 17.5   22.7 / 25.6    37.3 / 37.9    53.5 / 51.9   115.2 / 106.7   161.8 / 150.3 / 151.4   255.0 / 244.5 / 247.1   509 / 498 / 511
+// 384 MB kept: 320 MB 150.0 and 151.3, 512 MB 240.7 and 242.8 (the norm itself 83.5), 1 GB 495 and 497 (157).  bf16 differs by up to 2 %.
+inline uint64_t norm_keeps(uint64_t bytes, bool in_place) { return in_place && bytes < 80ull << 20 ? 0 : 256ull << 20; }
+
+// Clipping: whether the scaling adds the partials up itself, in each wave, which saves a launch, but where nothing is to be scaled each wave
+// would only have to read the factor.  us, a launch of its own / in the scaling, one binary32 tensor (bf16 is within 5 %):
+//                  1 MB         8 MB          16 MB         32 MB         48 MB         64 MB         96 MB         256 MB
+//   clipped       9.6 / 7.2   11.0 / 10.1   15.3 / 14.6   23.4 / 21.9   31.0 / 29.5   38.2 / 36.7   51.7 / 50.2   120.6 / 119.4
+//   below limit   9.4 / 7.2    9.6 / 7.3    11.8 / 9.4    11.6 / 11.2   14.3 / 14.4   16.9 / 17.5   23.9 / 25.2    52.6 / 58.5
+inline bool finish_in_scaling(uint64_t bytes) { return bytes <= 64ull << 20; }
 
 struct Range {
   uintptr_t begin, end;

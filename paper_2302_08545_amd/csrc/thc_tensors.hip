@@ -54,17 +54,11 @@ uint32_t run_partials(const thc_tensors* t, const Scan& scan, bool in_place, dou
           a.keep = kept;
           a.before = written;
         },
-        [&](const auto& a) { k_norm<KIND><<<dim3(groups), dim3(TNT), 0, s>>>(a); });
+        [&](const auto& a) { k_norm<KIND><<<dim3(groups), dim3(NORM_NT), 0, s>>>(a); });
     keep -= kept;
     written = groups > written ? groups : written;
   });
   return written;
-}
-
-template <int KIND>
-void run_final(const FinalArgs& f, hipStream_t s) {
-  if (f.count <= 1024) k_norm_final<KIND, 256, 4><<<dim3(1), dim3(256), 0, s>>>(f);
-  else k_norm_final<KIND, FINAL_NT, NORM_PARTIALS / FINAL_NT><<<dim3(1), dim3(FINAL_NT), 0, s>>>(f);
 }
 
 // whether the list goes through one launch of one workgroup; if so, that is done
@@ -100,14 +94,15 @@ void run_moves(const thc_tensors* t, const Scan& scan, Grid grid, uint32_t flat_
 template <int KIND>
 void run_norm(const thc_tensors* t, const Scan& scan, NormOut o, double* partials, hipStream_t s) {
   if (run_one<KIND>(t, scan, false, o, s)) return;
-  run_final<KIND>(FinalArgs{o, partials, run_partials<KIND>(t, scan, false, partials, s)}, s);
+  const FinalArgs f{o, partials, run_partials<KIND>(t, scan, false, partials, s)};
+  k_norm_final<KIND><<<dim3(1), dim3(NORM_PARTIALS), 0, s>>>(f);
 }
 
 template <int KIND>
 void run_clip(const thc_tensors* t, const Scan& scan, NormOut o, double* partials, hipStream_t s) {
   if (run_one<KIND>(t, scan, true, o, s)) return;
   const uint32_t written = run_partials<KIND>(t, scan, true, partials, s);
-  if (written <= FUSED_PARTIALS) {
+  if (finish_in_scaling(scan.bytes)) {
     for_tables(t, scan, Grid::TENSOR, 0, 0, LOG_MOVE_UNIT, [&](const TensorTable<TABLE>& tab, uint32_t count, uint32_t units) {
       with_table<FinishArgs>(
           tab, count,
@@ -120,7 +115,7 @@ void run_clip(const thc_tensors* t, const Scan& scan, NormOut o, double* partial
     });
     return;
   }
-  run_final<KIND>(FinalArgs{o, partials, written}, s);
+  k_norm_final<KIND><<<dim3(1), dim3(NORM_PARTIALS), 0, s>>>(FinalArgs{o, partials, written});
   run_moves(t, scan, Grid::TENSOR, 0, 0, nullptr, o.scale, [&](const auto& a, dim3 grid) { k_scale<<<grid, dim3(TNT), 0, s>>>(a); });
 }
 

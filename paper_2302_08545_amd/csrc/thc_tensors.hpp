@@ -5,7 +5,7 @@
 //   moves    y = round(fl32(x * c)): the product rounded to binary32, then to the type, as elementary operations would
 //
 // Bound by memory, with one operation per element (the norm: a conversion and a multiply-add in binary64, a quarter of the ALU at full
-// rate); small lists by launches.  Rates of large lists (MI355X; a copy reaches 6.0 TB/s): the norm reads 6.8 TB/s, moves 6.0 to 6.4.
+// rate); small lists by launches.  Rates of large lists (MI355X; a copy reaches 6.0 TB/s): the norm reads 7.0 TB/s, moves 6.0 to 6.4.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -16,11 +16,10 @@
 
 namespace thc {
 
-constexpr int TNT = 256;                   // threads per workgroup
-// Most workgroups of a norm launch, one partial each: 3.1 GB in bf16 467 us with 2048, 461 with 8192, 460 with 16384 (672 MB 110.4 / 109.1 /
-// 110.7).
-constexpr uint32_t NORM_PARTIALS = 8192;
-constexpr int FINAL_NT = 1024, ONE_NT = 1024;
+constexpr int TNT = 256;                   // threads per workgroup of a move
+// A norm launch has at most one workgroup, and one partial, for each of the GPU's 256 compute units.
+constexpr int NORM_NT = 512, ONE_NT = 1024;
+constexpr uint32_t NORM_PARTIALS = 256;
 
 struct Bf16 { uint16_t bits; };
 struct F16 { _Float16 v; };
@@ -133,11 +132,22 @@ template <> struct Acc<THC_NORM_MAX> {
   }
 };
 
+template <int CTRL>
+__device__ __forceinline__ double dpp(double v) {
+  const uint64_t w = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_mov_dpp((int)w, CTRL, 0xF, 0xF, true), hi = (uint32_t)__builtin_amdgcn_mov_dpp((int)(w >> 32), CTRL, 0xF, 0xF, true);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+
+// Fixed order; every lane gets the total.  The first four exchanges pair lanes, pairs, fours and eights inside a row of 16.
 template <int KIND>
 __device__ __forceinline__ double wave_join(double v) {
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) v = Acc<KIND>::join(v, __shfl_xor(v, m, 64));
-  return v;
+  v = Acc<KIND>::join(v, dpp<0xB1>(v));    // lane ^ 1
+  v = Acc<KIND>::join(v, dpp<0x4E>(v));    // lane ^ 2
+  v = Acc<KIND>::join(v, dpp<0x141>(v));   // the other four of eight
+  v = Acc<KIND>::join(v, dpp<0x140>(v));   // the other eight of sixteen
+  v = Acc<KIND>::join(v, __shfl_xor(v, 16, 64));
+  return Acc<KIND>::join(v, __shfl_xor(v, 32, 64));
 }
 
 // fixed order; every thread of the workgroup gets the total
@@ -204,15 +214,14 @@ struct NormArgs {
 };
 static_assert(sizeof(NormArgs<TensorTable<TABLE>>) <= 4096, "kernel arguments");
 
-// Seven workgroups to a compute unit: with registers for eight the magnitudes' form spills (672 MB of f16 125 us instead of 109).
 template <int KIND, class Table>
-__global__ __launch_bounds__(TNT, 7) void k_norm(const NormArgs<Table> a) {
+__global__ __launch_bounds__(NORM_NT) void k_norm(const NormArgs<Table> a) {
   Acc<KIND> acc;
   for (uint32_t u = blockIdx.x; u < a.units; u += gridDim.x) {
     const Piece p = locate<LOG_NORM_UNIT, Grid::TENSOR, 0>(a.tab, u);
-    norm_unit<LOG_NORM_UNIT, TNT>(p, u < a.keep, acc);
+    norm_unit<LOG_NORM_UNIT, NORM_NT>(p, u < a.keep, acc);
   }
-  const double v = group_join<KIND, TNT>(acc.get());
+  const double v = group_join<KIND, NORM_NT>(acc.get());
   if (threadIdx.x == 0) a.partials[blockIdx.x] = blockIdx.x < a.before ? Acc<KIND>::join(a.partials[blockIdx.x], v) : v;
 }
 
@@ -225,8 +234,11 @@ struct NormOut {
 // the factor that clips, from the sum of squares or the largest magnitude; one thread of the launch writes both
 template <int KIND>
 __device__ __forceinline__ float finish(const NormOut& o, double v, bool writes) {
+  const double limit = o.max_norm;
+  // a sum that exceeds the limit's square by less than its root's rounding has the factor 1 too, by way of the quotient
+  if (!writes && v <= (KIND == THC_NORM_L2 ? limit * limit : limit)) return 1.f;
   const double norm = KIND == THC_NORM_L2 ? __builtin_sqrt(v) : v;
-  const float c = norm <= (double)o.max_norm ? 1.f : (float)((double)o.max_norm / norm);
+  const float c = norm <= limit ? 1.f : (float)(limit / norm);
   if (writes) {
     *o.norm = (float)norm;
     if (o.scale) *o.scale = c;
@@ -240,19 +252,10 @@ struct FinalArgs {
   uint32_t count;
 };
 
-// N threads take up to PER partials each
-template <int KIND, int N, int PER>
-__global__ __launch_bounds__(N) void k_norm_final(const FinalArgs a) {
-  double x[PER];
-#pragma unroll
-  for (int k = 0; k < PER; ++k) {
-    const uint32_t i = threadIdx.x + k * N;
-    x[k] = i < a.count ? a.partials[i] : 0.0;
-  }
-  double v = x[0];
-#pragma unroll
-  for (int k = 1; k < PER; ++k) v = Acc<KIND>::join(v, x[k]);
-  finish<KIND>(a.out, group_join<KIND, N>(v), threadIdx.x == 0);
+template <int KIND>
+__global__ __launch_bounds__(NORM_PARTIALS) void k_norm_final(const FinalArgs a) {
+  const double v = threadIdx.x < a.count ? a.partials[threadIdx.x] : 0.0;
+  finish<KIND>(a.out, group_join<KIND, NORM_PARTIALS>(v), threadIdx.x == 0);
 }
 
 // ---- moves --------------------------------------------------------------------------------------------------------
@@ -318,10 +321,7 @@ struct MoveArgs {
 };
 static_assert(sizeof(MoveArgs<TensorTable<TABLE>>) <= 4096, "kernel arguments");
 
-// The scaling behind up to FUSED_PARTIALS partials, which each wave adds up by itself: the launch of k_norm_final is saved.  Clipping of one
-// binary32 tensor, us without / with: 256 KB 5.9 / 4.5, 2 MB 6.6 / 5.3, 8 MB (257 partials) 7.1 / 6.2, 16 MB (513) 8.5 / 8.6.
-constexpr uint32_t FUSED_PARTIALS = 384;
-
+// The same with the partials added up by each wave: the launch of k_norm_final is saved (see finish_in_scaling).
 template <class Table>
 struct FinishArgs {
   Table tab;
@@ -333,12 +333,12 @@ struct FinishArgs {
 template <int KIND, class Table>
 __global__ __launch_bounds__(TNT, 8) void k_finish_scale(const FinishArgs<Table> a) {
   const uint32_t lane = threadIdx.x & 63u;
-  double x[FUSED_PARTIALS / 64];
+  double x[NORM_PARTIALS / 64];
 #pragma unroll
-  for (uint32_t k = 0; k < FUSED_PARTIALS / 64; ++k) x[k] = lane + 64 * k < a.count ? a.partials[lane + 64 * k] : 0.0;
+  for (uint32_t k = 0; k < NORM_PARTIALS / 64; ++k) x[k] = lane + 64 * k < a.count ? a.partials[lane + 64 * k] : 0.0;
   double v = x[0];
 #pragma unroll
-  for (uint32_t k = 1; k < FUSED_PARTIALS / 64; ++k) v = Acc<KIND>::join(v, x[k]);
+  for (uint32_t k = 1; k < NORM_PARTIALS / 64; ++k) v = Acc<KIND>::join(v, x[k]);
   const float c = finish<KIND>(a.out, wave_join<KIND>(v), blockIdx.x == 0 && threadIdx.x == 0);
   if (c == 1.f) return;
   scale_piece<LOG_MOVE_UNIT, TNT>(locate<LOG_MOVE_UNIT, Grid::TENSOR, 0>(a.tab, blockIdx.x), c);

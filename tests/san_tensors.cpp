@@ -174,8 +174,9 @@ int main() {
     }
   }
   check_long();
-  check(norm_keeps(63ull << 20, true) == 0 && norm_keeps(64ull << 20, true) == 256ull << 20 && norm_keeps(1, false) == 256ull << 20 &&
-            norm_keeps((768ull << 20) - 1, false) == 256ull << 20 && norm_keeps(768ull << 20, true) == 384ull << 20, "norm_keeps");
+  check(norm_keeps((80ull << 20) - 1, true) == 0 && norm_keeps(80ull << 20, true) == 256ull << 20 && norm_keeps(1, false) == 256ull << 20,
+        "norm_keeps");
+  check(finish_in_scaling(64ull << 20) && !finish_in_scaling((64ull << 20) + 1), "finish_in_scaling");
   std::printf("%d problem(s)\n", problems);
   return problems != 0;
 }
