@@ -115,6 +115,13 @@ inline uint64_t norm_keeps(uint64_t bytes, bool in_place) { return in_place && b
 //   below limit   9.4 / 7.2    9.6 / 7.3    11.8 / 9.4    11.6 / 11.2   14.3 / 14.4   16.9 / 17.5   23.9 / 25.2    52.6 / 58.5
 inline bool finish_in_scaling(uint64_t bytes) { return bytes <= 64ull << 20; }
 
+// Shared memory that a move of a long list asks for and does not use: 26000 of a compute unit's 160 KB let six workgroups run there instead
+// of eight, and memory answers fewer accesses at a time faster.  us, nothing asked for / 26000 / 32000 bytes (six, five workgroups):
+// one tensor of 512 MB gather binary32 174.3 / 168.1 / 165.4, bf16 171.5 / 169.2 / 165.7, scatter 172.3 / 166.1 / 166.1, to bf16
+// 255.1 / 251.2 / 247.8, clip 244.0 / 242.2 / 241.4; scatter of VGG16's gradient 177.6 / 175.1 / 174.6; gather of GPT-2 XL's 1040 / 1036 /
+// 1052, which five are too few for.  At 160 MB gather gains 2 %, at 128 MB nothing; scatter to bf16 loses 1.5 % at 64 and 96 MB.
+inline uint32_t move_lds(uint64_t bytes) { return bytes > 128ull << 20 ? 26000 : 0; }
+
 struct Range {
   uintptr_t begin, end;
   Range(const void* p, uint64_t bytes) : begin(reinterpret_cast<uintptr_t>(p)), end(begin + (p ? bytes : 0)) {}

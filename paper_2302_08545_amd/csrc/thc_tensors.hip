@@ -116,7 +116,8 @@ void run_clip(const thc_tensors* t, const Scan& scan, NormOut o, double* partial
     return;
   }
   k_norm_final<KIND><<<dim3(1), dim3(NORM_PARTIALS), 0, s>>>(FinalArgs{o, partials, written});
-  run_moves(t, scan, Grid::TENSOR, 0, 0, nullptr, o.scale, [&](const auto& a, dim3 grid) { k_scale<<<grid, dim3(TNT), 0, s>>>(a); });
+  const uint32_t lds = move_lds(scan.bytes);
+  run_moves(t, scan, Grid::TENSOR, 0, 0, nullptr, o.scale, [&](const auto& a, dim3 grid) { k_scale<<<grid, dim3(TNT), lds, s>>>(a); });
 }
 
 int check_flat(const thc_params* p, const thc_tensors* t, const void* flat, uint32_t flat_bytes, const float* scale,
@@ -172,9 +173,10 @@ int thc_gather(const thc_params* p, const thc_tensors* t, const float* scale, vo
   const int rc = check_flat(p, t, grad_out, bytes, scale, false, &scan);
   if (rc) return rc;
   hipStream_t s = static_cast<hipStream_t>(stream);
+  const uint32_t lds = move_lds(scan.bytes);
   run_moves(t, scan, Grid::FLAT, bytes, p->d - scan.total, grad_out, scale, [&](const auto& a, dim3 grid) {
-    if (bytes == 2) k_gather<Bf16><<<grid, dim3(TNT), 0, s>>>(a);
-    else k_gather<float><<<grid, dim3(TNT), 0, s>>>(a);
+    if (bytes == 2) k_gather<Bf16><<<grid, dim3(TNT), lds, s>>>(a);
+    else k_gather<float><<<grid, dim3(TNT), lds, s>>>(a);
   });
   return check_launch();
 }
@@ -184,8 +186,9 @@ int thc_scatter(const thc_params* p, const float* flat, const float* scale, cons
   const int rc = check_flat(p, t, flat, 4, scale, true, &scan);
   if (rc) return rc;
   hipStream_t s = static_cast<hipStream_t>(stream);
+  const uint32_t lds = move_lds(scan.bytes);
   run_moves(t, scan, Grid::TENSOR, 0, 0, const_cast<float*>(flat), scale,
-            [&](const auto& a, dim3 grid) { k_scatter<<<grid, dim3(TNT), 0, s>>>(a); });
+            [&](const auto& a, dim3 grid) { k_scatter<<<grid, dim3(TNT), lds, s>>>(a); });
   return check_launch();
 }
 
