@@ -70,6 +70,7 @@ struct Scan {
   uint64_t total = 0, bytes = 0, entries = 0;
   uintptr_t begin = ~(uintptr_t)0, end = 0;   // all tensors lie between these
   bool ascending = true;                      // in the order of their addresses, none over another
+  bool wide = false, narrow = false;          // whether any element has four bytes, and two
 };
 
 inline int scan_tensors(const thc_tensors* t, Scan* out) {
@@ -92,28 +93,40 @@ inline int scan_tensors(const thc_tensors* t, Scan* out) {
     last = a + bytes;
     s.end = std::max(s.end, last);
     type = t->dtype[i];
+    (type == TYPE_F32 ? s.wide : s.narrow) = true;
     if (s.total > AT_MASK) return THC_EINVAL;
   }
   *out = s;
   return THC_OK;
 }
 
+// whether all elements have that size
+inline bool same_size(const Scan& s, uint32_t bytes) { return !(bytes == 4 ? s.narrow : s.wide); }
+
 // Bytes at the start of a list that the norm's pass reads with plain loads, so that the 256 MB memory-side cache holds them for the
 // call that moves the list next; the rest is read non-temporally, which is 7 % faster and does not push out what is kept.
-// us on one binary32 tensor, nothing kept / 256 MB kept / all kept:
-//              16 MB         32 MB          64 MB          96 MB         224 MB          320 MB                  512 MB                  1 GB
-//   norm      8.1 / 8.1    10.0 / 10.5    14.3 / 15.5    18.9 / 20.4    37.1 / 39.9     51.0 / 53.9 / 54.7      78.6 / 81.8 / 86.0      152 / 155 / 169
-//   + gather 16.7 / 14.5   23.8 / 21.0    38.4 / 35.1    53.3 / 48.9   113.3 / 104.8   159.1 / 147.6 / 149.9   253.3 / 241.4 / 245.5   507 / 496 / 509
-//   clip     14.7 / 17.5   22.7 / 25.6    37.3 / 37.9    53.5 / 51.9   115.2 / 106.7   161.8 / 150.3 / 151.4   255.0 / 244.5 / 247.1   509 / 498 / 511
-// 384 MB kept: 320 MB 150.0 and 151.3, 512 MB 240.7 and 242.8 (the norm itself 83.5), 1 GB 495 and 497 (157).  bf16 differs by up to 2 %.
-inline uint64_t norm_keeps(uint64_t bytes, bool in_place) { return in_place && bytes < 80ull << 20 ? 0 : 256ull << 20; }
+// us on one binary32 tensor, nothing kept / 256 MB kept (bf16 differs by up to 4 %):
+//              8 MB         16 MB          24 MB          32 MB          64 MB          96 MB         224 MB          512 MB           1 GB
+//   norm      8.1 / 8.0    8.1 / 8.0     8.7 / 8.9     9.8 / 10.6    14.1 / 15.3    18.7 / 20.2    37.1 / 39.7     78.5 / 81.2    152 / 155
+//   + gather 13.4 / 13.5  15.3 / 13.5   19.2 / 14.8   23.0 / 17.8    37.9 / 32.9    53.0 / 47.4   111.9 / 104.1   247.8 / 239.9   493 / 489
+//   clip     10.2 / 10.3  13.7 / 14.2   17.3 / 17.1   21.2 / 20.4    36.4 / 34.7    51.6 / 49.7   112.2 / 105.9   247.7 / 241.9   494 / 491
+inline uint64_t norm_keeps(uint64_t bytes, bool in_place) { return in_place && bytes < 24ull << 20 ? 0 : 256ull << 20; }
 
-// Clipping: whether the scaling adds the partials up itself, in each wave, which saves a launch, but where nothing is to be scaled each wave
-// would only have to read the factor.  us, a launch of its own / in the scaling, one binary32 tensor (bf16 is within 5 %):
-//                  1 MB         8 MB          16 MB         32 MB         48 MB         64 MB         96 MB         256 MB
-//   clipped       9.6 / 7.2   11.0 / 10.1   15.3 / 14.6   23.4 / 21.9   31.0 / 29.5   38.2 / 36.7   51.7 / 50.2   120.6 / 119.4
-//   below limit   9.4 / 7.2    9.6 / 7.3    11.8 / 9.4    11.6 / 11.2   14.3 / 14.4   16.9 / 17.5   23.9 / 25.2    52.6 / 58.5
-inline bool finish_in_scaling(uint64_t bytes) { return bytes <= 64ull << 20; }
+// Lists whose moves behind the norm go by its units of 32 KB: a unit is then read by the same one of the eight XCDs, whose L2 may still
+// have it, and clipping adds the partials up in each wave of the scaling, which saves a launch.  The rest goes by units of 8 KB, behind a
+// launch that adds the partials up.
+// us, units of 8 KB and that launch / units of 32 KB, one binary32 tensor (bf16 differs by up to 5 %):
+//                    4 MB          16 MB         32 MB         64 MB         96 MB         128 MB        160 MB          512 MB
+//   norm + gather  13.5 / 13.6  14.1 / 13.4   20.9 / 17.7   35.1 / 33.1   48.9 / 47.6   62.7 / 61.7   76.4 / 76.2   239.7 / 244.4
+//   clipped        11.6 / 9.8   18.7 / 14.6   27.2 / 20.3   39.0 / 34.8   51.7 / 49.8   64.7 / 64.0   78.3 / 78.4   242.2 / 248.2
+//   below limit    11.8 / 9.8   11.3 / 9.5    12.9 / 11.6   18.7 / 16.3   24.0 / 21.4   29.8 / 26.7   35.8 / 32.2    96.9 / 89.0
+// A gather by itself differs by up to 6 % one way or the other, and one that changes the size of its elements takes longer: those that are
+// given no factor, and those, go by 8 KB whatever their length.
+inline bool behind_norm(uint64_t bytes) { return bytes <= 128ull << 20; }
+
+// Shared memory that these gathers ask for and do not use: three workgroups run on a compute unit instead of five.  Norm and gather of
+// ResNet-50's gradients, us by bytes asked for, none / 32000 / 40000 / 53000: 56.7 / 55.8 / 54.8 / 54.0.
+constexpr uint32_t BEHIND_NORM_LDS = 53000;
 
 // Shared memory that a move of a long list asks for and does not use: 26000 of a compute unit's 160 KB let six workgroups run there instead
 // of eight, and memory answers fewer accesses at a time faster.  us, nothing asked for / 26000 / 32000 bytes (six, five workgroups):

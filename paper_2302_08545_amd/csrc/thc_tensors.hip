@@ -79,8 +79,9 @@ bool run_one(const thc_tensors* t, const Scan& scan, bool in_place, NormOut o, h
 }
 
 template <class Launch>
-void run_moves(const thc_tensors* t, const Scan& scan, Grid grid, uint32_t flat_bytes, uint64_t zeros, void* flat, const float* scale, Launch&& launch) {
-  for_tables(t, scan, grid, flat_bytes, zeros, LOG_MOVE_UNIT, [&](const TensorTable<TABLE>& tab, uint32_t count, uint32_t units) {
+void run_moves(const thc_tensors* t, const Scan& scan, Grid grid, uint32_t flat_bytes, uint64_t zeros, uint32_t log_unit, void* flat,
+               const float* scale, Launch&& launch) {
+  for_tables(t, scan, grid, flat_bytes, zeros, log_unit, [&](const TensorTable<TABLE>& tab, uint32_t count, uint32_t units) {
     with_table<MoveArgs>(
         tab, count,
         [&](auto& a) {
@@ -102,8 +103,8 @@ template <int KIND>
 void run_clip(const thc_tensors* t, const Scan& scan, NormOut o, double* partials, hipStream_t s) {
   if (run_one<KIND>(t, scan, true, o, s)) return;
   const uint32_t written = run_partials<KIND>(t, scan, true, partials, s);
-  if (finish_in_scaling(scan.bytes)) {
-    for_tables(t, scan, Grid::TENSOR, 0, 0, LOG_MOVE_UNIT, [&](const TensorTable<TABLE>& tab, uint32_t count, uint32_t units) {
+  if (behind_norm(scan.bytes)) {
+    for_tables(t, scan, Grid::TENSOR, 0, 0, LOG_NORM_UNIT, [&](const TensorTable<TABLE>& tab, uint32_t count, uint32_t units) {
       with_table<FinishArgs>(
           tab, count,
           [&](auto& a) {
@@ -117,7 +118,7 @@ void run_clip(const thc_tensors* t, const Scan& scan, NormOut o, double* partial
   }
   k_norm_final<KIND><<<dim3(1), dim3(NORM_PARTIALS), 0, s>>>(FinalArgs{o, partials, written});
   const uint32_t lds = move_lds(scan.bytes);
-  run_moves(t, scan, Grid::TENSOR, 0, 0, nullptr, o.scale, [&](const auto& a, dim3 grid) { k_scale<<<grid, dim3(TNT), lds, s>>>(a); });
+  run_moves(t, scan, Grid::TENSOR, 0, 0, LOG_MOVE_UNIT, nullptr, o.scale, [&](const auto& a, dim3 grid) { k_scale<<<grid, dim3(TNT), lds, s>>>(a); });
 }
 
 int check_flat(const thc_params* p, const thc_tensors* t, const void* flat, uint32_t flat_bytes, const float* scale,
@@ -173,10 +174,18 @@ int thc_gather(const thc_params* p, const thc_tensors* t, const float* scale, vo
   const int rc = check_flat(p, t, grad_out, bytes, scale, false, &scan);
   if (rc) return rc;
   hipStream_t s = static_cast<hipStream_t>(stream);
+  const uint64_t zeros = p->d - scan.total;
+  if (scale && same_size(scan, bytes) && behind_norm(scan.bytes)) {
+    run_moves(t, scan, Grid::FLAT, bytes, zeros, LOG_NORM_UNIT, grad_out, scale, [&](const auto& a, dim3 grid) {
+      if (bytes == 2) k_gather<LOG_NORM_UNIT, Bf16><<<grid, dim3(TNT), BEHIND_NORM_LDS, s>>>(a);
+      else k_gather<LOG_NORM_UNIT, float><<<grid, dim3(TNT), BEHIND_NORM_LDS, s>>>(a);
+    });
+    return check_launch();
+  }
   const uint32_t lds = move_lds(scan.bytes);
-  run_moves(t, scan, Grid::FLAT, bytes, p->d - scan.total, grad_out, scale, [&](const auto& a, dim3 grid) {
-    if (bytes == 2) k_gather<Bf16><<<grid, dim3(TNT), lds, s>>>(a);
-    else k_gather<float><<<grid, dim3(TNT), lds, s>>>(a);
+  run_moves(t, scan, Grid::FLAT, bytes, zeros, LOG_MOVE_UNIT, grad_out, scale, [&](const auto& a, dim3 grid) {
+    if (bytes == 2) k_gather<LOG_MOVE_UNIT, Bf16><<<grid, dim3(TNT), lds, s>>>(a);
+    else k_gather<LOG_MOVE_UNIT, float><<<grid, dim3(TNT), lds, s>>>(a);
   });
   return check_launch();
 }
@@ -187,7 +196,7 @@ int thc_scatter(const thc_params* p, const float* flat, const float* scale, cons
   if (rc) return rc;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const uint32_t lds = move_lds(scan.bytes);
-  run_moves(t, scan, Grid::TENSOR, 0, 0, const_cast<float*>(flat), scale,
+  run_moves(t, scan, Grid::TENSOR, 0, 0, LOG_MOVE_UNIT, const_cast<float*>(flat), scale,
             [&](const auto& a, dim3 grid) { k_scatter<<<grid, dim3(TNT), lds, s>>>(a); });
   return check_launch();
 }

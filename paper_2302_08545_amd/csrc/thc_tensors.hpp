@@ -293,10 +293,10 @@ __device__ __forceinline__ void move_unit(const S* src, D* dst, const Piece& p, 
 }
 
 // zeros, likewise
-template <class D>
+template <uint32_t LOG_UNIT, class D>
 __device__ __forceinline__ void zero_unit(D* dst, const Piece& p) {
-  constexpr int V = 16 / sizeof(D), K = (1 << LOG_MOVE_UNIT) / 16 / TNT;
-  const int64_t e = edge<LOG_MOVE_UNIT, TNT, 16, sizeof(D)>(p);
+  constexpr int V = 16 / sizeof(D), K = (1 << LOG_UNIT) / 16 / TNT;
+  const int64_t e = edge<LOG_UNIT, TNT, 16, sizeof(D)>(p);
   if (e >= 0) dst[e >> (sizeof(D) / 2)] = D{};
 #pragma unroll
   for (int k = 0; k < K; ++k) {
@@ -321,7 +321,7 @@ struct MoveArgs {
 };
 static_assert(sizeof(MoveArgs<TensorTable<TABLE>>) <= 4096, "kernel arguments");
 
-// The same with the partials added up by each wave: the launch of k_norm_final is saved (see finish_in_scaling).
+// Scaling with the partials added up by each wave: the launch of k_norm_final is saved (see behind_norm).
 template <class Table>
 struct FinishArgs {
   Table tab;
@@ -331,7 +331,7 @@ struct FinishArgs {
 };
 
 template <int KIND, class Table>
-__global__ __launch_bounds__(TNT, 8) void k_finish_scale(const FinishArgs<Table> a) {
+__global__ __launch_bounds__(TNT, 4) void k_finish_scale(const FinishArgs<Table> a) {
   const uint32_t lane = threadIdx.x & 63u;
   double x[NORM_PARTIALS / 64];
 #pragma unroll
@@ -341,7 +341,7 @@ __global__ __launch_bounds__(TNT, 8) void k_finish_scale(const FinishArgs<Table>
   for (uint32_t k = 1; k < NORM_PARTIALS / 64; ++k) v = Acc<KIND>::join(v, x[k]);
   const float c = finish<KIND>(a.out, wave_join<KIND>(v), blockIdx.x == 0 && threadIdx.x == 0);
   if (c == 1.f) return;
-  scale_piece<LOG_MOVE_UNIT, TNT>(locate<LOG_MOVE_UNIT, Grid::TENSOR, 0>(a.tab, blockIdx.x), c);
+  scale_piece<LOG_NORM_UNIT, TNT>(locate<LOG_NORM_UNIT, Grid::TENSOR, 0>(a.tab, blockIdx.x), c);
 }
 
 template <class Table>
@@ -351,15 +351,21 @@ __global__ __launch_bounds__(TNT, 8) void k_scale(const MoveArgs<Table> a) {
   scale_piece<LOG_MOVE_UNIT, TNT>(locate<LOG_MOVE_UNIT, Grid::TENSOR, 0>(a.tab, blockIdx.x), c);
 }
 
-template <class D, class Table>
-__global__ __launch_bounds__(TNT, 8) void k_gather(const MoveArgs<Table> a) {
+// units of LOG_NORM_UNIT: lists whose elements have the vector's size
+template <uint32_t LOG_UNIT, class D, class Table>
+__global__ __launch_bounds__(TNT, LOG_UNIT == LOG_MOVE_UNIT ? 8 : 4) void k_gather(const MoveArgs<Table> a) {
+  constexpr bool WIDE = LOG_UNIT == LOG_MOVE_UNIT || sizeof(D) == 4, NARROW = LOG_UNIT == LOG_MOVE_UNIT || sizeof(D) == 2;
   const float c = a.scale ? *a.scale : 1.f;
-  const Piece p = locate<LOG_MOVE_UNIT, Grid::FLAT, sizeof(D)>(a.tab, blockIdx.x);
+  const Piece p = locate<LOG_UNIT, Grid::FLAT, sizeof(D)>(a.tab, blockIdx.x);
   D* const dst = static_cast<D*>(a.flat) + p.at;
-  if (p.type == TYPE_F32) move_unit<LOG_MOVE_UNIT, TNT>(reinterpret_cast<const float*>(p.ptr), dst, p, c);
-  else if (p.type == TYPE_BF16) move_unit<LOG_MOVE_UNIT, TNT>(reinterpret_cast<const Bf16*>(p.ptr), dst, p, c);
-  else if (p.type == TYPE_F16) move_unit<LOG_MOVE_UNIT, TNT>(reinterpret_cast<const F16*>(p.ptr), dst, p, c);
-  else zero_unit(dst, p);
+  if (p.type == TYPE_ZEROS) zero_unit<LOG_UNIT>(dst, p);
+  if constexpr (WIDE) {
+    if (p.type == TYPE_F32) move_unit<LOG_UNIT, TNT>(reinterpret_cast<const float*>(p.ptr), dst, p, c);
+  }
+  if constexpr (NARROW) {
+    if (p.type == TYPE_BF16) move_unit<LOG_UNIT, TNT>(reinterpret_cast<const Bf16*>(p.ptr), dst, p, c);
+    else if (p.type == TYPE_F16) move_unit<LOG_UNIT, TNT>(reinterpret_cast<const F16*>(p.ptr), dst, p, c);
+  }
 }
 
 template <class Table>

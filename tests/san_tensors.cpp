@@ -150,7 +150,13 @@ int main() {
     check_cover(l, Grid::TENSOR, 0, 0, LOG_WAVE_UNIT, 16);
     check_cover(l, Grid::TENSOR, 0, 0, LOG_MOVE_UNIT, 8);
     for (uint32_t b : {2u, 4u}) check_cover(l, Grid::FLAT, b, zeros, LOG_MOVE_UNIT, round % 2 ? 16 : 8);
+    for (uint32_t b : {2u, 4u}) check_cover(l, Grid::FLAT, b, zeros, LOG_NORM_UNIT, 16);
     const thc_tensors t = l.get();
+    Scan scan;
+    bool wide = false, narrow = false;
+    for (uint64_t i = 0; i < t.count; ++i)
+      if (t.numel[i]) (t.dtype[i] == THC_DTYPE_F32 ? wide : narrow) = true;
+    check(scan_tensors(&t, &scan) == THC_OK && same_size(scan, 4) == !narrow && same_size(scan, 2) == !wide, "sizes of elements");
     check(overlap(&t, true, {}) == THC_OK, "overlap where there is none");
     if (count > 1) {                           // in another order, and then one of them twice
       std::swap(l.data.front(), l.data.back());
@@ -174,9 +180,9 @@ int main() {
     }
   }
   check_long();
-  check(norm_keeps((80ull << 20) - 1, true) == 0 && norm_keeps(80ull << 20, true) == 256ull << 20 && norm_keeps(1, false) == 256ull << 20,
+  check(norm_keeps((24ull << 20) - 1, true) == 0 && norm_keeps(24ull << 20, true) == 256ull << 20 && norm_keeps(1, false) == 256ull << 20,
         "norm_keeps");
-  check(finish_in_scaling(64ull << 20) && !finish_in_scaling((64ull << 20) + 1), "finish_in_scaling");
+  check(behind_norm(128ull << 20) && !behind_norm((128ull << 20) + 1), "behind_norm");
   std::printf("%d problem(s)\n", problems);
   return problems != 0;
 }

@@ -240,6 +240,46 @@ def test_a_tensor_of_more_than_2_to_the_32_elements():
     assert [float(x[k]) for k in spots] == [v / 2 for v in spots.values()] and int(torch.count_nonzero(x)) == 5
 
 
+@pytest.mark.parametrize("types", [(F32,), (BF16,), (F16, F32)], ids=["f32", "bf16", "mixed"])
+@pytest.mark.parametrize("over", [-1, 0, 1], ids=["below", "at", "above"])
+@pytest.mark.parametrize("tensors", [1, 250])
+def test_lists_around_128_mb(tensors, over, types):
+    left, parts = (128 << 20) + 4 * over, []
+    for i in range(tensors):
+        dtype = types[i % len(types)]
+        n = left // dtype.itemsize if i == tensors - 1 else (128 << 20) // tensors // dtype.itemsize - 5 * (i % 3)
+        left -= n * dtype.itemsize
+        # the same steps from a start of its own, so that no two places hold the same
+        parts.append(((torch.arange(n, device=DEV, dtype=torch.int32) * 40_503 + i * 977) % 2039 - 1019).to(F32).mul_(2.0 ** -12).to(dtype))
+    assert left < 4
+    before = [x.clone() for x in parts]
+    v = math.sqrt(math.fsum(float(x.double().square().sum()) for x in parts))
+    norm, scale, ws = _scalars()
+    total = sum(x.numel() for x in parts)
+    for out in (F32, BF16):
+        d = -(-total // 1024) * 1024 + 4096
+        p = api.make_params(d, 1024, 1, 4, 15, 2.0, 7, range(16), in_dtype=api.THC_DTYPE_BF16 if out == BF16 else api.THC_DTYPE_F32)
+        flat = torch.full((d,), 5.0, dtype=out, device=DEV)
+        api.thc_grad_norm(parts, api.THC_NORM_L2, v * 0.37, norm, scale, ws)
+        assert abs(float(norm) - v) <= v * NORM_REL
+        api.thc_gather(p, parts, scale, flat)
+        pos = 0
+        for x in before:
+            assert torch.equal(flat[pos:pos + x.numel()], (x.float() * scale).to(out))
+            pos += x.numel()
+        assert not bool(flat[total:].any())
+    api.thc_grad_clip(parts, api.THC_NORM_L2, v * 1.01, norm, scale, ws)
+    assert float(scale) == 1.0 and all(torch.equal(x, y) for x, y in zip(parts, before))
+    api.thc_grad_clip(parts, api.THC_NORM_L2, v * 0.37, norm, scale, ws)
+    assert all(torch.equal(x, (y.float() * scale).to(y.dtype)) for x, y in zip(parts, before))
+    est = torch.randn(d, device=DEV)
+    api.thc_scatter(p, est, scale, parts)
+    pos = 0
+    for x in parts:
+        assert torch.equal(x, (est[pos:pos + x.numel()] * scale).to(x.dtype))
+        pos += x.numel()
+
+
 def test_captured_and_replayed_with_eager_work_between():
     cpu = _values([5000, 7, 90_000, 1, 8192], (F32, BF16), seed=11)
     X = Tensors(cpu)
