@@ -5,7 +5,7 @@
 //   moves    y = round(fl32(x * c)): the product rounded to binary32, then to the type, as elementary operations would
 //
 // Bound by memory, with one operation per element (the norm: a conversion and a multiply-add in binary64, a quarter of the ALU at full
-// rate); small lists by launches.  Rates of large lists (MI355X; a copy reaches 6.0 TB/s): the norm reads 7.0 TB/s, moves 6.0 to 6.4.
+// rate); small lists by launches.  Rates of large lists (MI355X; a copy reaches 6.0 TB/s): the norm reads 7.0 TB/s, moves 6.0 to 6.5.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -380,9 +380,9 @@ __global__ __launch_bounds__(TNT, 8) void k_scatter(const MoveArgs<Table> a) {
 
 // ---- small lists ----------------------------------------------------------------------------------------------------
 // One workgroup, a unit to a wave, takes a list through the norm and, with SCALE, the scaling.  With up to two units a wave it is done
-// before two more launches would be.  us, this / the launches: binary32, 4 KB in one tensor 2.5 / 4.1 (with the scaling 2.4 / 5.7),
-// 64 KB in 8 3.1 / 4.7 (3.0 / 6.2), 128 KB in one 3.9 / 4.3 (3.8 / 5.9); bf16 128 KB 4.7 / 4.6 (4.8 / 6.2); three units a wave: 4 KB
-// in 48 tensors 5.5 / 4.8 (5.4 / 6.3), bf16 6.7 / 5.1 (7.2 / 6.7); four: 256 KB 5.3 / 4.5 (5.2 / 5.9).
+// before the two launches would be.  us, this / the launches: binary32, 4 KB in one tensor 2.3 / 3.8 (with the scaling 2.2 / 3.8), 64 KB in 8
+// 2.8 / 4.2 (2.6 / 4.3), 128 KB in one 3.6 / 3.9 (3.4 / 3.9); bf16 128 KB 4.4 / 4.0 (4.5 / 4.3), in 8 4.3 / 4.4 (4.4 / 4.6); three units a
+// wave: 4 KB in 48 tensors 5.3 / 4.2 (5.2 / 4.5), bf16 6.6 / 4.7 (7.1 / 4.9); four: 256 KB 5.2 / 4.0 (5.0 / 4.2).
 constexpr uint32_t ONE_MOST_UNITS = 2 * ONE_NT / 64;
 
 struct OneArgs {
