@@ -244,6 +244,8 @@ def make_tensors(tensors: Sequence) -> thc_tensors:
     if len(devices) > 1:
         raise ValueError("make_tensors: all tensors have to be on one device")
     for t in ts:
+        if t.is_neg():
+            raise ValueError("make_tensors: a tensor's memory holds its negative (part of a conjugate): resolve_neg() first")
         if not t.is_contiguous() and not _one_run(t):
             raise ValueError(f"make_tensors: a tensor of shape {tuple(t.shape)} with strides {tuple(t.stride())} is not one "
                              "run of memory")
@@ -253,27 +255,31 @@ def make_tensors(tensors: Sequence) -> thc_tensors:
     return out
 
 
+def _current_device() -> int:
+    try:
+        return _torch()._C._cuda_getDevice()
+    except AttributeError:                       # a name of torch's own that a build may lack
+        return _TORCH.cuda.current_device()
+
+
 def _list_and_stream(tensors, stream, where: str):
-    """The list as the library takes it, and the stream's handle.  The current stream is the current device's: the tensors
-    have to be there too."""
+    """The list as the library takes it, the stream's handle, and the device (None: not known).  The current stream is the
+    current device's: the tensors have to be there too."""
     t = tensors if type(tensors) is thc_tensors else make_tensors(tensors)
-    if stream is None and t.device is not None:
-        try:
-            current = _TORCH._C._cuda_getDevice()
-        except AttributeError:                   # a name of torch's own that a build may lack
-            current = _TORCH.cuda.current_device()
-        if current != t.device:
-            raise ValueError(f"{where}: the tensors are on cuda:{t.device}, the current device is cuda:{current}")
-        try:
-            return t, _TORCH._C._cuda_getCurrentRawStream(current)
-        except AttributeError:
-            pass
-    return t, _stream(stream)
+    if stream is not None:
+        return t, _stream(stream), t.device
+    current = _current_device()
+    if t.device is not None and current != t.device:
+        raise ValueError(f"{where}: the tensors are on cuda:{t.device}, the current device is cuda:{current}")
+    try:
+        return t, _TORCH._C._cuda_getCurrentRawStream(current), current
+    except AttributeError:
+        return t, _stream(None), current
 
 
-def _buffer(b, name: str, where: str, count: int, dtype: Optional[int]) -> Optional[int]:
-    """The address of a tensor on the GPU that has to hold `count` elements of a type (None: bytes) in one run; addresses as
-    they are."""
+def _buffer(b, name: str, where: str, count: int, dtype: Optional[int], device: Optional[int]) -> Optional[int]:
+    """The address of a tensor on the call's GPU that has to hold `count` elements of a type (None: bytes) in one run;
+    addresses as they are."""
     if b is None or type(b) is int:
         return b
     if dtype is None:
@@ -281,9 +287,9 @@ def _buffer(b, name: str, where: str, count: int, dtype: Optional[int]) -> Optio
     else:
         _torch()
         ok = b.numel() >= count and _DTYPES.get(b.dtype) == dtype
-    if not (ok and b.is_cuda and b.is_contiguous()):
-        raise ValueError(f"{where}: {name} has to be a contiguous tensor on the GPU with room for {count} "
-                         f"{'bytes' if dtype is None else 'values of its type'}")
+    if not (ok and b.is_contiguous() and (b.is_cuda if device is None else b.get_device() == device)):
+        raise ValueError(f"{where}: {name} has to be a contiguous tensor on {'the GPU' if device is None else f'cuda:{device}'} "
+                         f"with room for {count} {'bytes' if dtype is None else 'values of its type'}")
     return b.data_ptr()
 
 
@@ -300,9 +306,9 @@ def _norm_call(call, where: str, tensors, kind, max_norm, norm_out, scale_out, w
     global _NORM_WS
     if not _NORM_WS:
         _NORM_WS = thc_norm_workspace_bytes()
-    t, stream = _list_and_stream(tensors, stream, where)
-    rc = call(t, kind, max_norm, _buffer(norm_out, "norm_out", where, 1, THC_DTYPE_F32),
-              _buffer(scale_out, "scale_out", where, 1, THC_DTYPE_F32), _buffer(ws, "ws", where, _NORM_WS, None), stream)
+    t, stream, at = _list_and_stream(tensors, stream, where)
+    rc = call(t, kind, max_norm, _buffer(norm_out, "norm_out", where, 1, THC_DTYPE_F32, at),
+              _buffer(scale_out, "scale_out", where, 1, THC_DTYPE_F32, at), _buffer(ws, "ws", where, _NORM_WS, None, at), stream)
     if rc != 0:
         raise ThcError(rc, where)
 
@@ -320,16 +326,16 @@ def thc_grad_clip(tensors, kind: int, max_norm: float, norm_out, scale_out, ws, 
 
 def thc_gather(p: thc_params, tensors, scale, grad_out, stream=None) -> None:
     """The tensors one after another into the padded vector grad_out (p.d values of p.in_dtype), times *scale (None: 1)."""
-    t, stream = _list_and_stream(tensors, stream, "thc_gather")
-    _check((_LIB or lib()).thc_gather(p, t, _buffer(scale, "scale", "thc_gather", 1, THC_DTYPE_F32),
-                                      _buffer(grad_out, "grad_out", "thc_gather", p.d, p.in_dtype), stream), "thc_gather")
+    t, stream, at = _list_and_stream(tensors, stream, "thc_gather")
+    _check((_LIB or lib()).thc_gather(p, t, _buffer(scale, "scale", "thc_gather", 1, THC_DTYPE_F32, at),
+                                      _buffer(grad_out, "grad_out", "thc_gather", p.d, p.in_dtype, at), stream), "thc_gather")
 
 
 def thc_scatter(p: thc_params, flat, scale, tensors, stream=None) -> None:
     """The estimate `flat` (p.d float32 values) over the tensors, times *scale (None: 1)."""
-    t, stream = _list_and_stream(tensors, stream, "thc_scatter")
-    _check((_LIB or lib()).thc_scatter(p, _buffer(flat, "flat", "thc_scatter", p.d, THC_DTYPE_F32),
-                                       _buffer(scale, "scale", "thc_scatter", 1, THC_DTYPE_F32), t, stream), "thc_scatter")
+    t, stream, at = _list_and_stream(tensors, stream, "thc_scatter")
+    _check((_LIB or lib()).thc_scatter(p, _buffer(flat, "flat", "thc_scatter", p.d, THC_DTYPE_F32, at),
+                                       _buffer(scale, "scale", "thc_scatter", 1, THC_DTYPE_F32, at), t, stream), "thc_scatter")
 
 
 def thc_threshold(p: float) -> float:

@@ -185,6 +185,35 @@ def test_buffers_of_another_type_size_or_place_are_refused():
         api.thc_gather(_p(in_dtype=1), t, None, _gpu(torch.zeros(1 << 12)), stream=0)
 
 
+def test_buffers_of_another_device_than_the_lists_are_refused(monkeypatch):
+    here, there = _gpu(torch.zeros(1)), _gpu(torch.zeros(1), at=1)
+    ws = _gpu(torch.zeros(api.thc_norm_workspace_bytes(), dtype=torch.uint8))
+    far_ws = _gpu(torch.zeros(api.thc_norm_workspace_bytes(), dtype=torch.uint8), at=1)
+    flat, far = _gpu(torch.zeros(1 << 12)), _gpu(torch.zeros(1 << 12), at=1)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda d: 0, raising=False)
+    p = _p()
+    full = api.make_tensors([_gpu(torch.zeros(4))])
+    for t, stream in ((full, 0), (full, None), (api.make_tensors([]), None)):
+        for call in (api.thc_grad_norm, api.thc_grad_clip):
+            for norm, scale, work in ((there, here, ws), (here, there, ws), (here, None, far_ws)):
+                with pytest.raises(ValueError, match="cuda:0"):
+                    call(t, 0, 1.0, norm, scale, work, stream=stream)
+        for scale, vector in ((there, flat), (None, far)):
+            with pytest.raises(ValueError, match="cuda:0"):
+                api.thc_gather(p, t, scale, vector, stream=stream)
+            with pytest.raises(ValueError, match="cuda:0"):
+                api.thc_scatter(p, vector, scale, t, stream=stream)
+
+
+def test_a_tensor_whose_memory_holds_its_negative_is_refused():
+    x = torch.view_as_complex(torch.ones(1, 2)).conj().imag          # one element, -1, stored as 1
+    assert x.is_neg() and float(x) == -1.0
+    with pytest.raises(ValueError, match="negative"):
+        api.make_tensors([_gpu(x)])
+
+
 def test_tables_of_a_list_are_clean_under_asan_and_ubsan(tmp_path):
     """The tables that travel with the launches, walked on the CPU as the kernels walk them: every element once, nothing outside."""
     gxx = shutil.which("g++")
