@@ -243,9 +243,9 @@ int thc_norm_workspace_bytes(size_t* bytes_out /* host */);
 int thc_grad_norm(const thc_tensors* t, int kind, float max_norm, float* norm_out, float* scale_out /* or NULL */,
                   void* ws, void* stream);
 
-/* thc_grad_norm, and every element multiplied by the factor in binary32 and rounded to its type, in place.  Where
- * the factor is 1 nothing is written.  Tensors must not overlap each other (THC_EINVAL: a tensor listed twice would
- * be scaled twice). */
+/* thc_grad_norm (the same bits of norm and factor), and every element multiplied by the factor in binary32 and
+ * rounded to its type, in place.  Where the factor is 1 nothing is written.  Tensors must not overlap each other
+ * (THC_EINVAL: a tensor listed twice would be scaled twice). */
 int thc_grad_clip(const thc_tensors* t, int kind, float max_norm, float* norm_out, float* scale_out /* or NULL */,
                   void* ws, void* stream);
 

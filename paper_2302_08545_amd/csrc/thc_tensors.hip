@@ -96,7 +96,7 @@ template <int KIND>
 void run_norm(const thc_tensors* t, const Scan& scan, NormOut o, double* partials, hipStream_t s) {
   if (run_one<KIND>(t, scan, false, o, s)) return;
   const FinalArgs f{o, partials, run_partials<KIND>(t, scan, false, partials, s)};
-  k_norm_final<KIND><<<dim3(1), dim3(NORM_PARTIALS), 0, s>>>(f);
+  k_norm_final<KIND><<<dim3(1), dim3(64), 0, s>>>(f);
 }
 
 template <int KIND>
@@ -116,7 +116,7 @@ void run_clip(const thc_tensors* t, const Scan& scan, NormOut o, double* partial
     });
     return;
   }
-  k_norm_final<KIND><<<dim3(1), dim3(NORM_PARTIALS), 0, s>>>(FinalArgs{o, partials, written});
+  k_norm_final<KIND><<<dim3(1), dim3(64), 0, s>>>(FinalArgs{o, partials, written});
   const uint32_t lds = move_lds(scan.bytes);
   run_moves(t, scan, Grid::TENSOR, 0, 0, LOG_MOVE_UNIT, nullptr, o.scale, [&](const auto& a, dim3 grid) { k_scale<<<grid, dim3(TNT), lds, s>>>(a); });
 }

@@ -246,6 +246,19 @@ __device__ __forceinline__ float finish(const NormOut& o, double v, bool writes)
   return c;
 }
 
+// the partials added up by a wave, which gets the total in every lane
+template <int KIND>
+__device__ __forceinline__ double join_partials(const double* partials, uint32_t count) {
+  const uint32_t lane = threadIdx.x & 63u;
+  double x[NORM_PARTIALS / 64];
+#pragma unroll
+  for (uint32_t k = 0; k < NORM_PARTIALS / 64; ++k) x[k] = lane + 64 * k < count ? partials[lane + 64 * k] : 0.0;
+  double v = x[0];
+#pragma unroll
+  for (uint32_t k = 1; k < NORM_PARTIALS / 64; ++k) v = Acc<KIND>::join(v, x[k]);
+  return wave_join<KIND>(v);
+}
+
 struct FinalArgs {
   NormOut out;
   const double* partials;
@@ -253,9 +266,8 @@ struct FinalArgs {
 };
 
 template <int KIND>
-__global__ __launch_bounds__(NORM_PARTIALS) void k_norm_final(const FinalArgs a) {
-  const double v = threadIdx.x < a.count ? a.partials[threadIdx.x] : 0.0;
-  finish<KIND>(a.out, group_join<KIND, NORM_PARTIALS>(v), threadIdx.x == 0);
+__global__ __launch_bounds__(64) void k_norm_final(const FinalArgs a) {
+  finish<KIND>(a.out, join_partials<KIND>(a.partials, a.count), threadIdx.x == 0);
 }
 
 // ---- moves --------------------------------------------------------------------------------------------------------
@@ -332,14 +344,7 @@ struct FinishArgs {
 
 template <int KIND, class Table>
 __global__ __launch_bounds__(TNT, 4) void k_finish_scale(const FinishArgs<Table> a) {
-  const uint32_t lane = threadIdx.x & 63u;
-  double x[NORM_PARTIALS / 64];
-#pragma unroll
-  for (uint32_t k = 0; k < NORM_PARTIALS / 64; ++k) x[k] = lane + 64 * k < a.count ? a.partials[lane + 64 * k] : 0.0;
-  double v = x[0];
-#pragma unroll
-  for (uint32_t k = 1; k < NORM_PARTIALS / 64; ++k) v = Acc<KIND>::join(v, x[k]);
-  const float c = finish<KIND>(a.out, wave_join<KIND>(v), blockIdx.x == 0 && threadIdx.x == 0);
+  const float c = finish<KIND>(a.out, join_partials<KIND>(a.partials, a.count), blockIdx.x == 0 && threadIdx.x == 0);
   if (c == 1.f) return;
   scale_piece<LOG_NORM_UNIT, TNT>(locate<LOG_NORM_UNIT, Grid::TENSOR, 0>(a.tab, blockIdx.x), c);
 }

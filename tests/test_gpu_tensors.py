@@ -391,6 +391,17 @@ def test_clipping_without_a_place_for_the_factor(sizes):
     Y.guards_hold()
 
 
+@pytest.mark.parametrize("sizes", [[7, 300], [1000] * 33, [9_000_001, 13], [33_600_000, 5], [40] * 300 + [33_600_000]], ids=lambda s: f"{len(s)}x{s[-1]}")
+def test_norm_and_clip_give_the_same_bits(sizes):
+    for kind in (api.THC_NORM_L2, api.THC_NORM_MAX):
+        X = Tensors(_values(sizes, (F32,), seed=17))
+        one, c1, ws = _scalars()
+        two, c2, _ = _scalars()
+        api.thc_grad_norm(X.gpu, kind, 0.7, one, c1, ws)
+        api.thc_grad_clip(X.gpu, kind, 0.7, two, c2, ws)
+        assert torch.equal(one, two) and torch.equal(c1, c2) and 0.0 < float(c1) < 1.0
+
+
 def test_a_tensor_listed_twice_is_read_twice():
     x = torch.randn(10_000, generator=torch.Generator().manual_seed(8))
     g = x.to(DEV)
