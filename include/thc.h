@@ -233,9 +233,13 @@ int thc_norm_workspace_bytes(size_t* bytes_out /* host */);
 
 /* Global norm v over all elements of the list, and the factor that clips by it.
  *   max_norm   >= 0, may be infinite.
- *   norm_out   device, one float, written: v rounded once.  Squares are added up in binary64 in a fixed order (the
- *              same list at the same addresses modulo 128 bytes gives the same bits).  NaN if any element is NaN,
- *              else infinite if any element is, or if v exceeds binary32 (the factor then still goes by v itself).
+ *   norm_out   device, one float, written: v rounded once.  NaN if any element is NaN, else infinite if any
+ *              element is, or if v exceeds binary32 (the factor then still goes by v itself).  Squares are added up
+ *              in binary64, in an order that goes by the tensors' sizes, types and addresses modulo 128 bytes, and by
+ *              which of them adjoin (one starts where the last one with elements before it in the list ends, and has
+ *              its type: the two are then cut as one).  Lists that agree in all of that give the same bits; other
+ *              layouts of the same values may differ in the last one.  Processes that have to clip by exactly the
+ *              same factor therefore exchange it.
  *   scale_out  device, one float, written, or NULL: 1 where v <= max_norm, else max_norm / v rounded once (0 for
  *              infinite elements, NaN for NaN).
  * An empty list has norm 0 and factor 1.  To clip by a norm that covers more than this list (other processes'
