@@ -263,18 +263,29 @@ def _current_device() -> int:
 
 
 def _list_and_stream(tensors, stream, where: str):
-    """The list as the library takes it, the stream's handle, and the device (None: not known).  The current stream is the
-    current device's: the tensors have to be there too."""
+    """The list as the library takes it, the stream's handle, and the device (None: not known).  The tensors have to be on
+    the stream's device.  That is the current device for the current stream, and for the null stream (handles up to 2, as
+    legacy and per thread), which is the same number on every device; other streams say it themselves.  A bare handle of
+    such a stream does not: there the caller answers for it."""
     t = tensors if type(tensors) is thc_tensors else make_tensors(tensors)
-    if stream is not None:
-        return t, _stream(stream), t.device
-    current = _current_device()
-    if t.device is not None and current != t.device:
-        raise ValueError(f"{where}: the tensors are on cuda:{t.device}, the current device is cuda:{current}")
-    try:
-        return t, _TORCH._C._cuda_getCurrentRawStream(current), current
-    except AttributeError:
-        return t, _stream(None), current
+    what = "current device"
+    if stream is None:
+        at = _current_device()
+    else:
+        handle = _stream(stream)
+        if handle > 2:
+            device, what = getattr(stream, "device", None), "stream's device"
+            at = t.device if device is None else device.index
+        else:
+            at = _current_device() if t.device is not None or _torch().cuda.is_available() else None
+    if t.device is not None and at != t.device:
+        raise ValueError(f"{where}: the tensors are on cuda:{t.device}, the {what} is cuda:{at}")
+    if stream is None:
+        try:
+            handle = _TORCH._C._cuda_getCurrentRawStream(at)
+        except AttributeError:
+            handle = _stream(None)
+    return t, handle, at
 
 
 def _buffer(b, name: str, where: str, count: int, dtype: Optional[int], device: Optional[int]) -> Optional[int]:
