@@ -297,7 +297,7 @@ def _buffer(b, name: str, where: str, count: int, dtype: Optional[int], device: 
         ok = b.nbytes >= count
     else:
         _torch()
-        ok = b.numel() >= count and _DTYPES.get(b.dtype) == dtype
+        ok = b.numel() >= count and _DTYPES.get(b.dtype) == dtype and not b.is_neg()   # its memory then holds the negative
     if not (ok and b.is_contiguous() and (b.is_cuda if device is None else b.get_device() == device)):
         raise ValueError(f"{where}: {name} has to be a contiguous tensor on {'the GPU' if device is None else f'cuda:{device}'} "
                          f"with room for {count} {'bytes' if dtype is None else 'values of its type'}")

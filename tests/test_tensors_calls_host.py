@@ -44,3 +44,20 @@ def test_buffers_of_an_empty_list_have_to_be_on_the_streams_device(monkeypatch):
             for stream in (_stream(4096, 0), _stream(0, 0), 0):
                 with pytest.raises(ValueError, match="cuda:0"):
                     call([], 0, 1.0, norm, scale, ws, stream=stream)
+
+
+def test_buffers_whose_memory_holds_their_negative_are_refused():
+    x = _gpu(torch.view_as_complex(torch.ones(1, 2)).conj().imag)          # one float, -1, stored as 1
+    assert x.is_neg() and x.is_contiguous() and float(x) == -1.0
+    t, one, p = api.make_tensors([]), _gpu(torch.zeros(1)), _p()
+    ws = _gpu(torch.zeros(api.thc_norm_workspace_bytes(), dtype=torch.uint8))
+    flat = _gpu(torch.zeros(1 << 12))
+    for call in (api.thc_grad_norm, api.thc_grad_clip):
+        with pytest.raises(ValueError, match="norm_out"):
+            call(t, 0, 1.0, x, one, ws, stream=0)
+        with pytest.raises(ValueError, match="scale_out"):
+            call(t, 0, 1.0, one, x, ws, stream=0)
+    with pytest.raises(ValueError, match="scale"):
+        api.thc_gather(p, t, x, flat, stream=0)
+    with pytest.raises(ValueError, match="scale"):
+        api.thc_scatter(p, flat, x, t, stream=0)
