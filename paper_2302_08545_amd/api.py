@@ -31,10 +31,12 @@ class thc_params(C.Structure):
 
 
 class thc_tensors(C.Structure):
-    """A list of tensors as the library takes it; made by make_tensors, which keeps the tensors and their device with it."""
+    """A list of tensors as the library takes it; made by make_tensors, which keeps the tensors, the memory that they had then
+    and their device with it."""
     _fields_ = [("count", C.c_uint64), ("data", C.POINTER(C.c_void_p)), ("numel", C.POINTER(C.c_uint64)),
                 ("dtype", C.POINTER(C.c_uint32))]
     tensors: tuple = ()
+    storages: tuple = ()     # a tensor that is given other storage lets go of the memory that the list describes
     device: Optional[int] = None
 
 
@@ -227,8 +229,10 @@ def make_tensors(tensors: Sequence) -> thc_tensors:
     """Describes a list of GPU tensors (float32, bfloat16, float16; any mixture) for the calls below.
 
     Each tensor is taken in the order of its memory, so it has to be one run of memory: contiguous, or with its
-    dimensions in another order (channels last, transposed).  The list holds the tensors and the addresses that they
-    have now: keep it as long as they stay where they are, and make a new one when a gradient is replaced."""
+    dimensions in another order (channels last, transposed).  The list holds the tensors with the memory that they have
+    now, and goes on describing that memory: keep it as long as they stay where they are, and make a new one when a gradient
+    is replaced (as torch's zero_grad() does unless set_to_none=False) or given other storage (.data, set_).  Storage must
+    not be resized under it."""
     ts, n = tuple(tensors), 0
     _torch()
     try:                   # a training step may make a list of hundreds: each property of all of them in one go
@@ -237,6 +241,7 @@ def make_tensors(tensors: Sequence) -> thc_tensors:
         devices = {t.get_device() for t in ts}
         data = array("Q", [t.data_ptr() for t in ts])
         numel = array("Q", [t.numel() for t in ts])
+        storages = tuple([t.untyped_storage() for t in ts])
     except (AttributeError, KeyError, RuntimeError, TypeError):
         devices = {-1}
     if -1 in devices:
@@ -251,7 +256,7 @@ def make_tensors(tensors: Sequence) -> thc_tensors:
                              "run of memory")
     out = thc_tensors(n, (C.c_void_p * n).from_buffer(data), (C.c_uint64 * n).from_buffer(numel),
                       (C.c_uint32 * n).from_buffer(types)) if n else thc_tensors()
-    out.tensors, out.device = ts, devices.pop() if n else None
+    out.tensors, out.storages, out.device = ts, storages, devices.pop() if n else None
     return out
 
 

@@ -1,12 +1,15 @@
 """What the binding of the calls on lists checks before it hands raw addresses on: streams, devices, storage."""
+import gc
 import types
+import weakref
 
+import numpy as np
 import pytest
 import torch
 
 from paper_2302_08545_amd import api
 
-from .test_tensors_host import NORM, SCALE, WS, _gpu, _p
+from .test_tensors_host import NORM, SCALE, WS, _Gpu, _gpu, _p
 
 
 def _calls(t, **kw):
@@ -61,3 +64,20 @@ def test_buffers_whose_memory_holds_their_negative_are_refused():
         api.thc_gather(p, t, x, flat, stream=0)
     with pytest.raises(ValueError, match="scale"):
         api.thc_scatter(p, flat, x, t, stream=0)
+
+
+def test_a_list_keeps_the_memory_that_it_describes():
+    """A tensor that is given other storage leaves its addresses in the list: the memory there has to stay allocated."""
+    memory = np.zeros(64, dtype=np.float32)
+    seen, at = weakref.ref(memory), memory.ctypes.data
+    g = torch.Tensor._make_subclass(_Gpu, torch.from_numpy(memory))        # no view, which would keep the tensor it is of
+    t = api.make_tensors([g])
+    del memory
+    g.data = torch.ones(64)
+    gc.collect()
+    alive = seen() is not None
+    assert alive and t.data[0] == at
+    del t
+    gc.collect()
+    alive = seen() is not None
+    assert not alive
