@@ -112,20 +112,41 @@ inline bool same_size(const Scan& s, uint32_t bytes) { return !(bytes == 4 ? s.n
 //   clip     10.2 / 10.3  13.7 / 14.2   17.3 / 17.1   21.2 / 20.4    36.4 / 34.7    51.6 / 49.7   112.2 / 105.9   247.7 / 241.9   494 / 491
 inline uint64_t norm_keeps(uint64_t bytes, bool in_place) { return in_place && bytes < 24ull << 20 ? 0 : 256ull << 20; }
 
-// Lists whose moves behind the norm go by its units of 32 KB: a unit is then read by the same one of the eight XCDs, whose L2 may still
-// have it, and clipping adds the partials up in each wave of the scaling, which saves a launch.  The rest goes by units of 8 KB, behind a
-// launch that adds the partials up.
-// us, units of 8 KB and that launch / units of 32 KB, one binary32 tensor (bf16 differs by up to 5 %):
-//                    4 MB          16 MB         32 MB         64 MB         96 MB         128 MB        160 MB          512 MB
-//   norm + gather  13.5 / 13.6  14.1 / 13.4   20.9 / 17.7   35.1 / 33.1   48.9 / 47.6   62.7 / 61.7   76.4 / 76.2   239.7 / 244.4
-//   clipped        11.6 / 9.8   18.7 / 14.6   27.2 / 20.3   39.0 / 34.8   51.7 / 49.8   64.7 / 64.0   78.3 / 78.4   242.2 / 248.2
-//   below limit    11.8 / 9.8   11.3 / 9.5    12.9 / 11.6   18.7 / 16.3   24.0 / 21.4   29.8 / 26.7   35.8 / 32.2    96.9 / 89.0
-// A gather by itself differs by up to 6 % one way or the other, and one that changes the size of its elements takes longer: those that are
-// given no factor, and those, go by 8 KB whatever their length.
+// Lists that are scaled behind their norm by its units of 32 KB: a unit is then read by the same one of the eight XCDs, whose L2 may still
+// have it, and each wave of the scaling adds the partials up, which saves a launch.  The rest goes by units of 8 KB, behind a launch that
+// adds the partials up.  us, units of 8 KB and that launch / units of 32 KB, tensors of binary32 (bf16 differs by up to 5 %):
+//                         4 MB          16 MB         32 MB         51 MB         102 MB        127 MB        160 MB         512 MB
+//   clipped, one       11.1 / 10.2   15.7 / 14.1   26.2 / 20.6   34.4 / 27.5   54.3 / 49.6   64.2 / 60.9   78.3 / 78.4   242.2 / 248.2
+//   clipped, 400       22.3 / 21.0   25.3 / 25.7   34.5 / 32.6   41.8 / 38.2   64.3 / 59.2   74.8 / 69.8
+//   below limit, one   11.4 / 9.8    11.5 / 9.8    13.5 / 12.0   16.9 / 14.9   25.0 / 22.4   29.6 / 26.5   35.8 / 32.2    96.9 / 89.0
+//   below limit, 400   21.8 / 20.3   23.2 / 21.6   23.3 / 21.8   24.5 / 24.4   33.7 / 32.5   37.7 / 35.7
 inline bool behind_norm(uint64_t bytes) { return bytes <= 128ull << 20; }
 
-// Shared memory that these gathers ask for and do not use: three workgroups run on a compute unit instead of five.  Norm and gather of
-// ResNet-50's gradients, us by bytes asked for, none / 32000 / 40000 / 53000: 56.7 / 55.8 / 54.8 / 54.0.
+// Gathers by those units, for the same XCD's sake: those that are given a factor, which as a rule is that of a norm before them.
+// us, units of 8 KB / 32 KB, tensors:
+//                                 8 MB          12 MB         16 MB         32 MB         51 MB         102 MB        127 MB
+//   norm + gather, f32     1   12.2 / 12.0                 14.4 / 13.7   20.6 / 18.6   29.5 / 27.3   51.3 / 49.3   62.1 / 60.6
+//                        160   13.8 / 13.9   14.7 / 14.2   17.1 / 15.0   24.1 / 21.6   32.7 / 30.3   57.8 / 54.8   69.0 / 66.1
+//                        400                 23.4 / 23.7   24.8 / 24.7   32.5 / 32.7   41.0 / 41.8   65.1 / 65.4   76.7 / 76.5
+//                 bf16     1   12.4 / 12.2                 15.0 / 14.1   21.2 / 19.0   29.9 / 28.1   51.9 / 49.9   62.6 / 61.1
+//                        160   14.7 / 16.0   15.4 / 14.1   18.1 / 16.8   25.4 / 24.4   34.4 / 33.6   60.5 / 58.4   74.3 / 71.3
+//                        400                 25.0 / 26.1   26.3 / 28.1   34.1 / 37.4   43.2 / 46.6   67.9 / 71.6   82.4 / 85.0
+//   gather alone, f32    160    6.2 / 7.1     7.6 / 8.2     9.3 / 9.9    14.7 / 15.3   21.3 / 21.3   37.8 / 37.6   45.5 / 45.8
+//                 bf16   160    6.6 / 9.7     8.2 / 10.7    9.3 / 12.4   14.6 / 18.2   21.1 / 24.1   37.4 / 41.1   45.7 / 49.0
+//                        400                 12.5 / 18.0   13.6 / 19.6   19.1 / 24.4   24.8 / 30.8   42.6 / 49.0   50.2 / 56.5
+// Each launch of the large units costs some us that a second launch does not win back, so lists of more than one go by 8 KB, and so do
+// short ones, which win nothing behind a norm, and gathers that change the size of their elements, which take longer.  A gather of bf16 by
+// a factor with no norm before it is what the rule costs: up to 4 us.
+inline bool gather_behind_norm(const Scan& s, uint32_t flat_bytes, uint64_t zeros) {
+  return same_size(s, flat_bytes) && s.bytes >= 12ull << 20 && behind_norm(s.bytes) && s.entries + (zeros != 0) <= TABLE;
+}
+
+// Shared memory that these gathers ask for and do not use: three workgroups run on a compute unit instead of five.  us of norm and gather,
+// nothing asked for / 53000: binary32, 160 tensors 24 MB 18.4 / 18.5, 32 MB 22.2 / 21.6, 51 MB 33.0 / 30.3, 76 MB 45.6 / 42.7, 102 MB
+// 57.5 / 54.8, 127 MB 68.6 / 66.1, 40 tensors 51 MB 31.4 / 29.6, 127 MB 67.3 / 65.2; bf16, 160 tensors 51 MB 34.8 / 33.6, 102 MB 59.7 / 58.4,
+// 127 MB 72.6 / 71.3; one tensor of either type 32 MB 18.4 / 18.6 and 18.6 / 19.0, from 51 MB on the same.  By themselves these gathers differ
+// by up to 3 % one way or the other.  Asking for less does less: binary32, 160 tensors, 102 MB 57.1 / 56.8 / 55.5 / 54.7 with 26000 / 32000 /
+// 40000 / 53000.
 constexpr uint32_t BEHIND_NORM_LDS = 53000;
 
 // Shared memory that a move of a long list asks for and does not use: 26000 of a compute unit's 160 KB let six workgroups run there instead

@@ -175,7 +175,7 @@ int thc_gather(const thc_params* p, const thc_tensors* t, const float* scale, vo
   if (rc) return rc;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const uint64_t zeros = p->d - scan.total;
-  if (scale && same_size(scan, bytes) && behind_norm(scan.bytes)) {
+  if (scale && gather_behind_norm(scan, bytes, zeros)) {
     run_moves(t, scan, Grid::FLAT, bytes, zeros, LOG_NORM_UNIT, grad_out, scale, [&](const auto& a, dim3 grid) {
       if (bytes == 2) k_gather<LOG_NORM_UNIT, Bf16><<<grid, dim3(TNT), BEHIND_NORM_LDS, s>>>(a);
       else k_gather<LOG_NORM_UNIT, float><<<grid, dim3(TNT), BEHIND_NORM_LDS, s>>>(a);
