@@ -232,7 +232,8 @@ enum { THC_NORM_L2 = 0, THC_NORM_MAX = 1 };
 int thc_norm_workspace_bytes(size_t* bytes_out /* host */);
 
 /* Global norm v over all elements of the list, and the factor that clips by it.
- *   max_norm   >= 0, may be infinite.
+ *   max_norm   >= 0, may be infinite.  Binary32, so a limit computed in binary64 is rounded on the way in: the factor
+ *              is that of the limit as given here.
  *   norm_out   device, one float, written: v rounded once.  NaN if any element is NaN, else infinite if any
  *              element is, or if v exceeds binary32 (the factor then still goes by v itself).  Squares are added up
  *              in binary64, in an order that goes by the tensors' sizes, types and addresses modulo 128 bytes, and by

@@ -301,7 +301,8 @@ def _buffer(b, name: str, where: str, count: int, dtype: Optional[int], device: 
     if dtype is None:
         ok = b.nbytes >= count
     else:
-        _torch()
+        if _TORCH is None:
+            _torch()
         ok = b.numel() >= count and _DTYPES.get(b.dtype) == dtype and not b.is_neg()   # its memory then holds the negative
     if not (ok and b.is_contiguous() and (b.is_cuda if device is None else b.get_device() == device)):
         raise ValueError(f"{where}: {name} has to be a contiguous tensor on {'the GPU' if device is None else f'cuda:{device}'} "
@@ -331,7 +332,8 @@ def _norm_call(call, where: str, tensors, kind, max_norm, norm_out, scale_out, w
 
 def thc_grad_norm(tensors, kind: int, max_norm: float, norm_out, scale_out, ws, stream=None) -> None:
     """Global norm of a list of tensors (thc_tensors, or a sequence of tensors) and, unless scale_out is None, the factor
-    that clips it to max_norm; both are one float32 on the GPU."""
+    that clips it to max_norm; both are one float32 on the GPU.  max_norm is taken as float32: the factor is that of the
+    rounded limit, up to half a step (2^-24) off that of a Python float."""
     _norm_call((_LIB or lib()).thc_grad_norm, "thc_grad_norm", tensors, kind, max_norm, norm_out, scale_out, ws, stream)
 
 
