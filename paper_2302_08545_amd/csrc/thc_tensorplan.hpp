@@ -104,12 +104,14 @@ inline int scan_tensors(const thc_tensors* t, Scan* out) {
 inline bool same_size(const Scan& s, uint32_t bytes) { return !(bytes == 4 ? s.narrow : s.wide); }
 
 // Bytes at the start of a list that the norm's pass reads with plain loads, so that the 256 MB memory-side cache holds them for the
-// call that moves the list next; the rest is read non-temporally, which is 7 % faster and does not push out what is kept.
-// us on one binary32 tensor, nothing kept / 256 MB kept (bf16 differs by up to 4 %):
-//              8 MB         16 MB          24 MB          32 MB          64 MB          96 MB         224 MB          512 MB           1 GB
-//   norm      8.1 / 8.0    8.1 / 8.0     8.7 / 8.9     9.8 / 10.6    14.1 / 15.3    18.7 / 20.2    37.1 / 39.7     78.5 / 81.2    152 / 155
-//   + gather 13.4 / 13.5  15.3 / 13.5   19.2 / 14.8   23.0 / 17.8    37.9 / 32.9    53.0 / 47.4   111.9 / 104.1   247.8 / 239.9   493 / 489
-//   clip     10.2 / 10.3  13.7 / 14.2   17.3 / 17.1   21.2 / 20.4    36.4 / 34.7    51.6 / 49.7   112.2 / 105.9   247.7 / 241.9   494 / 491
+// call that moves the list next; the rest is read non-temporally, which is up to 9 % faster and does not push out what is kept.
+// us on one binary32 tensor, nothing kept / 256 MB kept (bf16 differs by up to 6 %):
+//              8 MB         16 MB         24 MB         32 MB         64 MB         96 MB         224 MB          512 MB           1 GB
+//   norm      5.8 / 5.9    6.9 / 7.3     8.2 / 8.7     9.3 / 10.0   13.9 / 15.0   18.4 / 20.0   36.7 / 39.5     78.1 / 81.0    152 / 155
+//   + gather 10.8 / 9.9   14.5 / 12.1   18.7 / 14.7   22.8 / 17.1   37.7 / 32.1   52.7 / 46.7   110.9 / 103.7   247.6 / 239.2   493 / 487
+//   clip      8.9 / 9.9   13.1 / 13.9   17.1 / 16.8   21.0 / 20.4   36.1 / 32.2   51.2 / 47.4   112.3 / 105.3   247.8 / 242.4   493 / 490
+// A norm by itself pays up to 9 % for it.  That no factor is wanted from it tells nothing: norms of several lists may be combined, and the
+// list then moved by a factor of the caller's.
 inline uint64_t norm_keeps(uint64_t bytes, bool in_place) { return in_place && bytes < 24ull << 20 ? 0 : 256ull << 20; }
 
 // Lists that are scaled behind their norm by its units of 32 KB: a unit is then read by the same one of the eight XCDs, whose L2 may still

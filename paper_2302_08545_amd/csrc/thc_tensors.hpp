@@ -5,7 +5,7 @@
 //   moves    y = round(fl32(x * c)): the product rounded to binary32, then to the type, as elementary operations would
 //
 // Bound by memory, with one operation per element (the norm: a conversion and a multiply-add in binary64, a quarter of the ALU at full
-// rate); small lists by launches.  Rates of large lists (MI355X; a copy reaches 6.0 TB/s): the norm reads 7.0 TB/s, moves 6.0 to 6.5.
+// rate); small lists by launches.  Rates of large lists (MI355X): the norm reads 6.9 TB/s (7.3 from one tensor of 4 GB), moves 6.0 to 6.4.
 #pragma once
 
 #include <hip/hip_runtime.h>
