@@ -262,7 +262,7 @@ def make_tensors(tensors: Sequence) -> thc_tensors:
 
 def _current_device() -> int:
     try:
-        return _torch()._C._cuda_getDevice()
+        return (_TORCH or _torch())._C._cuda_getDevice()
     except AttributeError:                       # a name of torch's own that a build may lack
         return _TORCH.cuda.current_device()
 
@@ -273,18 +273,18 @@ def _list_and_stream(tensors, stream, where: str):
     legacy and per thread), which is the same number on every device; other streams say it themselves.  A bare handle of
     such a stream does not: there the caller answers for it."""
     t = tensors if type(tensors) is thc_tensors else make_tensors(tensors)
-    what = "current device"
+    own, whose = t.device, "current device"
     if stream is None:
         at = _current_device()
     else:
         handle = _stream(stream)
         if handle > 2:
-            device, what = getattr(stream, "device", None), "stream's device"
-            at = t.device if device is None else device.index
+            device, whose = getattr(stream, "device", None), "stream's device"
+            at = own if device is None else device.index
         else:
-            at = _current_device() if t.device is not None or _torch().cuda.is_available() else None
-    if t.device is not None and at != t.device:
-        raise ValueError(f"{where}: the tensors are on cuda:{t.device}, the {what} is cuda:{at}")
+            at = _current_device() if own is not None or _torch().cuda.is_available() else None
+    if own is not None and at != own:
+        raise ValueError(f"{where}: the tensors are on cuda:{own}, the {whose} is cuda:{at}")
     if stream is None:
         try:
             handle = _TORCH._C._cuda_getCurrentRawStream(at)
